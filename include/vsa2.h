@@ -16,6 +16,17 @@
  *   vsa2_attn_bwd  its gradients dQ, dK, dV with the block mask held fixed
  *                  (Sec. 2.1: the routing decision carries no gradient)
  *
+ * and what a model has to do around it:
+ *
+ *   vsa2_qk_norm_rope  per-head RMS norm of queries and keys, rotation by the
+ *                  token's (time, height, width) position and the cube-major
+ *                  layout of q, k and v in one pass; vsa2_qk_norm_rope_bwd
+ *                  its gradients
+ *   vsa2_cache_write, vsa2_cache_read  a paged 8-bit cache of the keys and
+ *                  values of earlier frames, for streaming generation
+ *   vsa2_attn_cache  attention of new tokens, one to whole frames of them,
+ *                  over that cache
+ *
  * Conventions shared by every call
  *   Memory     Every tensor pointer is a DEVICE pointer owned by the caller.
  *              The library never allocates device memory; calls that need
@@ -104,7 +115,8 @@ typedef enum {
     VSA2_ERR_ALIGN = 6,        /* a tensor pointer is not 16-byte aligned      */
     VSA2_ERR_WORKSPACE = 7,    /* workspace missing or smaller than required   */
     VSA2_ERR_HIP = 8,          /* a HIP launch failed                          */
-    VSA2_ERR_UNSUPPORTED = 9   /* valid but outside the supported shapes       */
+    VSA2_ERR_UNSUPPORTED = 9,  /* valid but outside the supported shapes       */
+    VSA2_ERR_VALUE = 10        /* a scalar argument outside its range          */
 } vsa2_status;
 
 typedef enum { VSA2_F32 = 0, VSA2_BF16 = 1 } vsa2_dtype;
@@ -447,6 +459,173 @@ vsa2_status vsa2_joint_lists(const vsa2_problem* p, const int32_t* row_ptr, cons
  */
 vsa2_status vsa2_unpool_add(const vsa2_problem* p, int32_t heads, const void* dx_c, int32_t Pt, int32_t Ph,
                             int32_t Pw, void* dx, hipStream_t stream);
+
+/*
+ * Rows of D contiguous elements, one per (sequence, head, token), as a
+ * projection leaves them: row (b, h, i) starts at ptr + b*batch + h*head +
+ * i*token (strides in elements, >= 0; the stride of an axis of size one is not
+ * looked at).  ptr is 16-byte aligned and every stride that is used a multiple
+ * of 16 bytes.  Input rows may share memory (a stride of 0); the rows that a
+ * call writes must not overlap (a stride of 0 there is VSA2_ERR_SHAPE).
+ */
+typedef struct {
+    void* ptr;
+    int64_t batch, head, token;
+} vsa2_rows;
+
+/*
+ * Rotary positions with up to three axes (time, height, width).
+ *   axis[a]   elements of a head that axis a turns (even, 0 = none); together
+ *             at most D.  Pair i = 0 .. (sum axis)/2 - 1 belongs to the axes in
+ *             order: the first axis[0]/2 pairs to time, and so on.
+ *   table[a]  device [rows[a]][axis[a]/2][2] fp32, (cos, sin) of each position's
+ *             angle for each pair of the axis; NULL where axis[a] = 0.
+ *   origin    device int32 [batch][3], the position of each sequence's first
+ *             grid token, or NULL for (0, 0, 0): the grid token (t, h, w) of
+ *             sequence b takes rows t + origin[b][0], h + origin[b][1] and
+ *             w + origin[b][2] of the tables.  A row outside a table is clamped
+ *             into it (never read); without origin the tables must cover the grid.
+ *   pairing   which elements pair i is: VSA2_ROPE_ADJACENT 2i and 2i + 1,
+ *             VSA2_ROPE_HALVES i and i + (sum axis)/2 (sum a multiple of 8).
+ * Elements past the pairs are not turned, nor are text tokens.
+ */
+typedef enum { VSA2_ROPE_ADJACENT = 0, VSA2_ROPE_HALVES = 1 } vsa2_rope_pairing;
+typedef struct {
+    int32_t axis[3];
+    int32_t rows[3];
+    const float* table[3];
+    const int32_t* origin;
+    int32_t pairing;     /* vsa2_rope_pairing */
+} vsa2_rope;
+
+/*
+ * vsa2_qk_norm_rope - for every token and head of the projected queries and keys
+ *   u = x / sqrt(mean(x^2) + eps) * gain      (eps = 0: no norm, u = x)
+ *   y = u with each pair (a, b) turned: (a cos - b sin, a sin + b cos)
+ * written in the library's cube-major token order; values are carried over as
+ * they are.  One pass: every input row is read once and every output row
+ * written once.  A head in fp32 registers from the read to the one rounding at
+ * the end.
+ *   q_in, k_in, v_in  rows (batch, heads_q or heads_kv, T*H*W + text_len tokens
+ *           in raster order, w fastest, then the text); parts of one fused
+ *           projection are such rows.
+ *   q, k, v  [batch][heads][L][D] ([Ljoint] with text), contiguous; padding
+ *           tokens are written as zeros.
+ *   Any of the three may be left out (its rows and its output both NULL).
+ *   q_gain, k_gain  fp32 [D] or NULL for ones (must be NULL with eps = 0).
+ *   r       NULL: no rotation.
+ * Any cube size is taken: with 1 x 1 x 1 cubes the order stays raster and
+ * there is no padding, the form for tokens that go into a cache.
+ * Errors: NULL pointers; eps negative or not finite, a gain with eps = 0, a
+ * pairing that is neither (VSA2_ERR_VALUE); an odd or negative axis, axes above
+ * D, a table shorter than the grid, negative strides (VSA2_ERR_SHAPE);
+ * misalignment; D not 64 or 128, more than 2^31 - 1 tokens (VSA2_ERR_UNSUPPORTED).
+ */
+vsa2_status vsa2_qk_norm_rope(const vsa2_problem* p, const vsa2_rope* r, float eps, const vsa2_rows* q_in,
+                              const float* q_gain, void* q, const vsa2_rows* k_in, const float* k_gain, void* k,
+                              const vsa2_rows* v_in, void* v, hipStream_t stream);
+
+/*
+ * vsa2_qk_norm_rope_bwd - gradients of vsa2_qk_norm_rope for dq, dk, dv (cube-
+ * major, contiguous; padding tokens are not looked at).  With g the gradient
+ * turned back, n = x / sqrt(mean(x^2) + eps) and h = g * gain,
+ *   dx = (h - n mean(h n)) / sqrt(mean(x^2) + eps),   dgain = sum g n
+ * over all tokens of all heads (g itself is dx with eps = 0).
+ *   q_in, k_in  as in the forward (not read, and may be NULL, with eps = 0)
+ *   dq_in, dk_in, dv_in  rows that receive the gradients of the projections,
+ *           the same rows (batch, heads, tokens) as the forward's inputs
+ *   dq_gain, dk_gain  fp32 [D], or NULL; summed in a fixed order
+ *   ws, ws_bytes  workspace of vsa2_qk_norm_rope_workspace bytes, 256-byte
+ *           aligned; only looked at when a gain's gradient is asked for.
+ *   Any of q, k, v may be left out (its dq / dq_in both NULL).
+ * Errors: as for vsa2_qk_norm_rope; a gain's gradient with eps = 0
+ * (VSA2_ERR_VALUE); workspace missing or too small.
+ */
+vsa2_status vsa2_qk_norm_rope_workspace(const vsa2_problem* p, size_t* bytes);
+vsa2_status vsa2_qk_norm_rope_bwd(const vsa2_problem* p, const vsa2_rope* r, float eps, const vsa2_rows* q_in,
+                                  const float* q_gain, const void* dq, const vsa2_rows* dq_in, float* dq_gain,
+                                  const vsa2_rows* k_in, const float* k_gain, const void* dk,
+                                  const vsa2_rows* dk_in, float* dk_gain, const void* dv, const vsa2_rows* dv_in,
+                                  void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * A paged key/value cache in 8 bits, for streaming generation.
+ *
+ * A page holds 64 tokens of one KV head: their keys and values as float8 e4m3
+ * codes and one power of two per token and tensor; value = code * 2^e.  The
+ * power is the smallest that brings the row's largest finite value to 448 or
+ * less (at least 2^-100), so a value keeps 4 significant bits down to 2^-13 of
+ * the row's largest, and reading back is exact in bf16.  A value that is
+ * not finite is stored as NaN.  (Values above 1.9375 * 2^127 read back infinite.)
+ *
+ * pool  device uint8 [pages][heads_kv][128 D + 128], 256-byte aligned.  One
+ *       page, in the order the matrix instructions take it (every read of the
+ *       attention is a run of whole 1 KB lines):
+ *         K codes  64 D bytes  [4 t][D/64 u][4 g][16 r][16 b]: token 16 t + r, element 64 u + 16 g + b
+ *         V codes  64 D bytes  [D/16 c][4 g][16 r][4 t][4 i]:  element 16 c + r, token 16 t + 4 g + i
+ *         K powers 64 bytes    [16 r][4 t], e + 127
+ *         V powers 64 bytes    [4 g][4 t][4 i], e + 127
+ * table device int32 [batch][table_heads][max_pages]: the pages of each
+ *       sequence's list in order; list position j is token j % 64 of page
+ *       table[j / 64].  table_heads is 1 (one list for all KV heads) or heads_kv
+ *       (every head has its own, as a router that picks pages per head gives).
+ *       Entries outside [0, pages) are skipped: nothing is written or read
+ *       there, and attention leaves those 64 positions out.
+ */
+typedef struct {
+    int32_t batch, heads_kv, head_dim;
+    int32_t pages, max_pages, table_heads;
+    void* pool;
+    const int32_t* table;
+} vsa2_cache;
+
+/* Bytes of one page of one KV head: 128 D + 128. */
+vsa2_status vsa2_cache_page_bytes(int32_t head_dim, size_t* bytes);
+
+/*
+ * vsa2_cache_write - quantise n tokens of every sequence into the cache: token
+ * i < min(n, count[b]) of sequence b goes to list position start[b] + i.  The
+ * rest of the pages keeps what it holds.
+ *   k, v   rows (batch, heads_kv, n) of dtype; keys normalised and rotated as
+ *          they will be used.
+ *   start  device int32 [batch]; positions outside [0, 64 max_pages) are
+ *          skipped.  count  device int32 [batch], or NULL for n.
+ * vsa2_cache_read - the reverse: the same positions into rows of dtype; places
+ *          past a count, outside the list or on a skipped page read as zeros.
+ * Errors: NULL pointers, dtype, negative sizes or strides, D not 64 or 128,
+ * table_heads neither 1 nor heads_kv, misalignment.  n = 0 does nothing.
+ */
+vsa2_status vsa2_cache_write(const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k, const vsa2_rows* v,
+                             const int32_t* start, const int32_t* count, hipStream_t stream);
+vsa2_status vsa2_cache_read(const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k, const vsa2_rows* v,
+                            const int32_t* start, const int32_t* count, hipStream_t stream);
+
+/*
+ * vsa2_attn_cache - attention of n new tokens of every sequence over its cached
+ * list: query head h (KV head h / (heads_q / heads_kv)) of token i attends
+ * list positions j < limit, softmax of q.k_j / sqrt(D), with
+ *   limit = length[b]                          (causal = 0)
+ *   limit = length[b] - (count[b] - 1 - i)     (causal = 1: the call's tokens are
+ *                                               the last count[b] of the list)
+ *   limit = 0 for i >= count[b].
+ *   dtype   of q and o; products are exact in the cached codes, and fp32
+ *           queries and probabilities enter them as three bf16 terms.
+ *   q, o    rows (batch, heads_q, n); o is written.
+ *   lse     [batch][heads_q][n] fp32 natural-log log-sum-exp.
+ *   length  device int32 [batch] (clamped to [0, 64 max_pages]); count device
+ *           int32 [batch] or NULL for n.
+ *   A row with nothing to attend gets o = 0, lse = -inf.  What masked places and
+ *   the pages' unwritten rest hold (NaN too) reaches no output.
+ *   ws, ws_bytes  workspace of vsa2_attn_cache_workspace bytes, 256-byte aligned:
+ *           partial results of long lists, which are split over workgroups and
+ *           joined in a fixed order.
+ * Errors: as for vsa2_cache_write; heads_q not a multiple of heads_kv
+ * (VSA2_ERR_SHAPE); workspace missing or too small.  n = 0 does nothing.
+ */
+vsa2_status vsa2_attn_cache_workspace(const vsa2_cache* c, int32_t heads_q, int32_t n, size_t* bytes);
+vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n, const vsa2_rows* q,
+                            const int32_t* length, const int32_t* count, int32_t causal, const vsa2_rows* o,
+                            float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * vsa2_mfma_peak_probe - a measurement aid, not part of the attention path:

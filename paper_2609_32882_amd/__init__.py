@@ -22,9 +22,10 @@ LIB_PATH = os.path.join(_PKG, "libvsa2.so")
 VSA2_OK = 0
 STATUS_NAMES = {0: "VSA2_OK", 1: "VSA2_ERR_NULL", 2: "VSA2_ERR_SHAPE", 3: "VSA2_ERR_DTYPE",
                 4: "VSA2_ERR_SELECT", 5: "VSA2_ERR_CAPACITY", 6: "VSA2_ERR_ALIGN",
-                7: "VSA2_ERR_WORKSPACE", 8: "VSA2_ERR_HIP", 9: "VSA2_ERR_UNSUPPORTED"}
+                7: "VSA2_ERR_WORKSPACE", 8: "VSA2_ERR_HIP", 9: "VSA2_ERR_UNSUPPORTED", 10: "VSA2_ERR_VALUE"}
 VSA2_F32, VSA2_BF16 = 0, 1
 VSA2_SEL_TOPK, VSA2_SEL_MASS, VSA2_SEL_SEQ_TOPK = 0, 1, 2
+VSA2_ROPE_ADJACENT, VSA2_ROPE_HALVES = 0, 1
 
 # Every symbol include/vsa2.h declares.
 EXPORTS = ("vsa2_status_str", "vsa2_pool", "vsa2_route_capacity", "vsa2_route_workspace",
@@ -32,6 +33,9 @@ EXPORTS = ("vsa2_status_str", "vsa2_pool", "vsa2_route_capacity", "vsa2_route_wo
            "vsa2_attn_bwd_prep", "vsa2_attn_bwd_dkdv", "vsa2_attn_bwd_dq",
            "vsa2_coarse_fwd", "vsa2_coarse_bwd", "vsa2_gate_merge", "vsa2_gate_merge_bwd",
            "vsa2_joint_capacity", "vsa2_joint_workspace", "vsa2_joint_lists", "vsa2_unpool_add",
+           "vsa2_qk_norm_rope", "vsa2_qk_norm_rope_workspace", "vsa2_qk_norm_rope_bwd",
+           "vsa2_cache_page_bytes", "vsa2_cache_write", "vsa2_cache_read",
+           "vsa2_attn_cache_workspace", "vsa2_attn_cache",
            "vsa2_mfma_peak_probe", "vsa2_dq_atomic_probe")
 
 
@@ -44,6 +48,22 @@ class vsa2_problem(ctypes.Structure):
 class vsa2_select(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int32), ("k", ctypes.c_int32), ("mass", ctypes.c_float),
                 ("cap", ctypes.c_int32)]
+
+
+class vsa2_rows(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("token", ctypes.c_int64)]
+
+
+class vsa2_rope(ctypes.Structure):
+    _fields_ = [("axis", ctypes.c_int32 * 3), ("rows", ctypes.c_int32 * 3), ("table", ctypes.c_void_p * 3),
+                ("origin", ctypes.c_void_p), ("pairing", ctypes.c_int32)]
+
+
+class vsa2_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("batch", "heads_kv", "head_dim", "pages", "max_pages", "table_heads")] + \
+               [("pool", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 class Vsa2Error(RuntimeError):
@@ -86,6 +106,16 @@ def _lib():
         L.vsa2_joint_capacity.argtypes = [pp, ps, ctypes.POINTER(i64)]
         L.vsa2_joint_workspace.argtypes = [pp, ctypes.POINTER(sz)]
         L.vsa2_joint_lists.argtypes = [pp, P, P, i64, P, P, i64, P, P, P, sz, P]
+        pr, pw, pc, f32 = (ctypes.POINTER(vsa2_rope), ctypes.POINTER(vsa2_rows), ctypes.POINTER(vsa2_cache),
+                           ctypes.c_float)
+        L.vsa2_qk_norm_rope.argtypes = [pp, pr, f32, pw, P, P, pw, P, P, pw, P, P]
+        L.vsa2_qk_norm_rope_workspace.argtypes = [pp, ctypes.POINTER(sz)]
+        L.vsa2_qk_norm_rope_bwd.argtypes = [pp, pr, f32, pw, P, P, pw, P, pw, P, P, pw, P, P, pw, P, sz, P]
+        L.vsa2_cache_page_bytes.argtypes = [i32, ctypes.POINTER(sz)]
+        L.vsa2_cache_write.argtypes = [pc, i32, i32, pw, pw, P, P, P]
+        L.vsa2_cache_read.argtypes = [pc, i32, i32, pw, pw, P, P, P]
+        L.vsa2_attn_cache_workspace.argtypes = [pc, i32, i32, ctypes.POINTER(sz)]
+        L.vsa2_attn_cache.argtypes = [pc, i32, i32, i32, pw, P, P, i32, pw, P, P, sz, P]
         L.vsa2_mfma_peak_probe.argtypes = [i32, P, ctypes.POINTER(i64), P]
         L.vsa2_dq_atomic_probe.argtypes = [pp, P, P, i64, P, P]
         for n in EXPORTS[1:]:
@@ -220,6 +250,49 @@ def vsa2_joint_lists(p, row_ptr, col_idx, col_cap, j_row_ptr, j_col_idx, j_cap, 
                      ws_bytes, stream=0):
     return _lib().vsa2_joint_lists(_ref(p), row_ptr, col_idx, col_cap, j_row_ptr, j_col_idx, j_cap,
                                    j_kv_ptr, j_kv_idx, ws, ws_bytes, stream)
+
+
+def vsa2_qk_norm_rope(p, r, eps, q_in, q_gain, q, k_in, k_gain, k, v_in, v, stream=0):
+    return _lib().vsa2_qk_norm_rope(_ref(p), _ref(r), eps, _ref(q_in), q_gain, q, _ref(k_in), k_gain, k,
+                                    _ref(v_in), v, stream)
+
+
+def vsa2_qk_norm_rope_workspace(p):
+    n = ctypes.c_size_t(0)
+    st = _lib().vsa2_qk_norm_rope_workspace(_ref(p), ctypes.byref(n))
+    return st, n.value
+
+
+def vsa2_qk_norm_rope_bwd(p, r, eps, q_in, q_gain, dq, dq_in, dq_gain, k_in, k_gain, dk, dk_in, dk_gain, dv, dv_in,
+                          ws, ws_bytes, stream=0):
+    return _lib().vsa2_qk_norm_rope_bwd(_ref(p), _ref(r), eps, _ref(q_in), q_gain, dq, _ref(dq_in), dq_gain,
+                                        _ref(k_in), k_gain, dk, _ref(dk_in), dk_gain, dv, _ref(dv_in), ws, ws_bytes,
+                                        stream)
+
+
+def vsa2_cache_page_bytes(head_dim):
+    n = ctypes.c_size_t(0)
+    st = _lib().vsa2_cache_page_bytes(head_dim, ctypes.byref(n))
+    return st, n.value
+
+
+def vsa2_cache_write(c, dtype, n, k, v, start, count, stream=0):
+    return _lib().vsa2_cache_write(_ref(c), dtype, n, _ref(k), _ref(v), start, count, stream)
+
+
+def vsa2_cache_read(c, dtype, n, k, v, start, count, stream=0):
+    return _lib().vsa2_cache_read(_ref(c), dtype, n, _ref(k), _ref(v), start, count, stream)
+
+
+def vsa2_attn_cache_workspace(c, heads_q, n):
+    b = ctypes.c_size_t(0)
+    st = _lib().vsa2_attn_cache_workspace(_ref(c), heads_q, n, ctypes.byref(b))
+    return st, b.value
+
+
+def vsa2_attn_cache(c, dtype, heads_q, n, q, length, count, causal, o, lse, ws, ws_bytes, stream=0):
+    return _lib().vsa2_attn_cache(_ref(c), dtype, heads_q, n, _ref(q), length, count, causal, _ref(o), lse, ws,
+                                  ws_bytes, stream)
 
 
 # --------------------------------------------------------------------------
@@ -502,3 +575,237 @@ def unpool_add(p, dx_c, dx, P):
     _check("vsa2_unpool_add", vsa2_unpool_add(p, dx.shape[1], dx_c.data_ptr(), P[0], P[1], P[2],
                                               dx.data_ptr(), _stream()))
     return dx
+
+
+# --------------------------------------------------------------------------
+# norm + rotation + layout, the 8-bit cache and attention over it
+# --------------------------------------------------------------------------
+
+def _rows(t, shape, dtype, name):
+    """vsa2_rows of t [batch, heads, tokens, D] with any strides but D's."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.stride(3) != 1:
+        raise ValueError("%s: expected %s %s on the GPU with contiguous rows, got %s %s strides %s" %
+                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape), tuple(t.stride())))
+    b, h, n, _ = t.stride()
+    return vsa2_rows(t.data_ptr(), b, h, n)
+
+
+def _int_vector(t, n, name):
+    """Pointer of an int32 GPU vector [n], or None."""
+    if t is None:
+        return None
+    _expect(t, (n,) if isinstance(n, int) else n, _torch().int32, name)
+    return t.data_ptr()
+
+
+def _gain(t, D, name):
+    if t is None:
+        return None
+    _expect(t, (D,), _torch().float32, name)
+    return t.data_ptr()
+
+
+def _vdtype(dtype):
+    torch = _torch()
+    if dtype == torch.bfloat16:
+        return VSA2_BF16
+    if dtype == torch.float32:
+        return VSA2_F32
+    raise ValueError("expected torch.bfloat16 or torch.float32, got %s" % dtype)
+
+
+def rope_table(rows, dims, theta=10000.0, device="cuda"):
+    """(cos, sin) [rows, dims/2, 2] fp32 of the angles position * theta^(-2 i / dims),
+    worked out in 64 bits; one axis of a Rope."""
+    torch = _torch()
+    freq = theta ** (-torch.arange(0, dims, 2, dtype=torch.float64) / dims)
+    angle = torch.arange(rows, dtype=torch.float64)[:, None] * freq
+    return torch.stack([angle.cos(), angle.sin()], -1).float().to(device)
+
+
+class Rope:
+    """Rotary positions over (time, height, width): `axes` elements of a head per
+    axis, one table per axis (None for an axis of 0 elements), the int32
+    [batch, 3] position of each sequence's first token (None: the grid's own),
+    and which elements pair up ("adjacent" or "halves")."""
+
+    __slots__ = ("c", "keep")
+
+    def __init__(self, axes, tables, origin=None, pairing="adjacent"):
+        torch = _torch()
+        c = vsa2_rope(pairing={"adjacent": VSA2_ROPE_ADJACENT, "halves": VSA2_ROPE_HALVES}[pairing])
+        for i, (n, t) in enumerate(zip(axes, tables)):
+            c.axis[i] = n
+            if n:
+                _expect(t, (t.shape[0], n // 2, 2), torch.float32, "tables[%d]" % i)
+                c.rows[i], c.table[i] = t.shape[0], t.data_ptr()
+        if origin is not None:
+            _expect(origin, (origin.shape[0], 3), torch.int32, "origin")
+            c.origin = origin.data_ptr()
+        self.c, self.keep = c, (tables, origin)
+
+    def check(self, p):
+        origin = self.keep[1]
+        if origin is not None and origin.shape[0] != p.batch:
+            raise ValueError("origin: expected %d sequences, got %d" % (p.batch, origin.shape[0]))
+        return self.c
+
+
+def _rope_c(rope, p):
+    return None if rope is None else rope.check(p)
+
+
+def _raster(p):
+    """Tokens of a sequence before the cube-major layout: the grid, then the text."""
+    return p.T * p.H * p.W + p.text_len
+
+
+def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None, eps=0.0, out=None):
+    """Per-head RMS norm (eps > 0) of q and k with their gains, rotation, and the
+    cube-major layout of all three: q [batch, heads_q, tokens, D], k and v
+    [batch, heads_kv, tokens, D] in raster order (views of a fused projection
+    are fine), each may be None.  Returns (q, k, v) contiguous; `out` gives the
+    three outputs."""
+    torch = _torch()
+    p = problem_from(p)
+    dt, n, L, D = _tdtype(p), _raster(p), _joint(p)[1], p.head_dim
+    rows, ptrs, outs = [], [], []
+    for i, (x, name) in enumerate(((q, "q"), (k, "k"), (v, "v"))):
+        if x is None:
+            rows.append(None), ptrs.append(None), outs.append(None)
+            continue
+        heads = p.heads_kv if i else p.heads_q
+        rows.append(_rows(x, (p.batch, heads, n, D), dt, name))
+        if out is not None:
+            y = out[i]
+            _expect(y, (p.batch, heads, L, D), dt, "out[%d]" % i)
+        else:
+            y = torch.empty((p.batch, heads, L, D), dtype=dt, device=x.device)
+        outs.append(y)
+        ptrs.append(y.data_ptr())
+    _check("vsa2_qk_norm_rope", vsa2_qk_norm_rope(p, _rope_c(rope, p), eps, rows[0], _gain(q_gain, D, "q_gain"),
+                                                  ptrs[0], rows[1], _gain(k_gain, D, "k_gain"), ptrs[1], rows[2],
+                                                  ptrs[2], _stream()))
+    return tuple(outs)
+
+
+def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, k_gain=None, rope=None, eps=0.0,
+                     out=None):
+    """Gradients of qk_norm_rope for dq, dk, dv (contiguous, cube-major; each may
+    be None): (dq_in, dk_in, dv_in, dq_gain, dk_gain), the first three like the
+    forward's inputs ([batch, heads, tokens, D]; `out` gives them, views of one
+    fused gradient are fine).  q and k are the forward's inputs, needed with the
+    norm; the gains' gradients come with them."""
+    torch = _torch()
+    p = problem_from(p)
+    dt, n, L, D = _tdtype(p), _raster(p), _joint(p)[1], p.head_dim
+    norm = eps > 0
+    dy, dx, dx_rows, x_rows, dgain = [], [], [], [], []
+    for i, (g, x, name) in enumerate(((dq, q, "q"), (dk, k, "k"), (dv, None, "v"))):
+        if g is None:
+            dy.append(None), dx.append(None), dx_rows.append(None), x_rows.append(None), dgain.append(None)
+            continue
+        heads = p.heads_kv if i else p.heads_q
+        _expect(g, (p.batch, heads, L, D), dt, "d" + name)
+        y = out[i] if out is not None else torch.empty((p.batch, n, heads, D), dtype=dt, device=g.device).transpose(1, 2)
+        dy.append(g.data_ptr())
+        dx.append(y)
+        dx_rows.append(_rows(y, (p.batch, heads, n, D), dt, "out[%d]" % i))
+        x_rows.append(_rows(x, (p.batch, heads, n, D), dt, name) if x is not None else None)
+        dgain.append(torch.empty(D, dtype=torch.float32, device=g.device) if norm and i < 2 else None)
+    wsb, ws = 0, None
+    if dgain[0] is not None or dgain[1] is not None:
+        st, wsb = vsa2_qk_norm_rope_workspace(p)
+        _check("vsa2_qk_norm_rope_workspace", st)
+        ws = torch.empty(wsb, dtype=torch.uint8, device=(dx[0] if dx[0] is not None else dx[1]).device)
+    _check("vsa2_qk_norm_rope_bwd", vsa2_qk_norm_rope_bwd(
+        p, _rope_c(rope, p), eps, x_rows[0], _gain(q_gain, D, "q_gain"), dy[0], dx_rows[0], _ptr(dgain[0]),
+        x_rows[1], _gain(k_gain, D, "k_gain"), dy[1], dx_rows[1], _ptr(dgain[1]), dy[2], dx_rows[2], _ptr(ws), wsb,
+        _stream()))
+    return dx[0], dx[1], dx[2], dgain[0], dgain[1]
+
+
+class KVCache:
+    """A paged 8-bit key/value cache: `pool` uint8 [pages, heads_kv, 128*D + 128]
+    and `table` int32 [batch, max_pages], or [batch, heads_kv, max_pages] with a
+    list of pages for every KV head (include/vsa2.h has the page's layout)."""
+
+    __slots__ = ("c", "pool", "table")
+
+    def __init__(self, pool, table):
+        torch = _torch()
+        if pool.dim() != 3 or (pool.shape[2] - 128) % 128:
+            raise ValueError("pool: expected [pages, heads_kv, 128*D + 128], got %s" % (tuple(pool.shape),))
+        _expect(pool, pool.shape, torch.uint8, "pool")
+        _expect(table, table.shape, torch.int32, "table")
+        pages, heads = pool.shape[0], pool.shape[1]
+        if table.dim() == 2:
+            per_head = 1
+        elif table.dim() == 3 and table.shape[1] == heads:
+            per_head = heads
+        else:
+            raise ValueError("table: expected [batch, max_pages] or [batch, %d, max_pages], got %s" %
+                             (heads, tuple(table.shape)))
+        self.c = vsa2_cache(table.shape[0], heads, (pool.shape[2] - 128) // 128, pages, table.shape[-1], per_head,
+                            pool.data_ptr(), table.data_ptr())
+        self.pool, self.table = pool, table
+
+    @classmethod
+    def empty(cls, table, pages, heads_kv, head_dim):
+        """A cache of `pages` pages with nothing in them, on the table's GPU."""
+        st, b = vsa2_cache_page_bytes(head_dim)
+        _check("vsa2_cache_page_bytes", st)
+        return cls(_torch().empty((pages, heads_kv, b), dtype=_torch().uint8, device=table.device), table)
+
+
+def cache_write(cache, k, v, start, count=None):
+    """Quantise tokens k, v [batch, heads_kv, n, D] (any strides) into the cache:
+    token i < count[b] (int32 [batch], None: all n) goes to list position
+    start[b] + i (int32 [batch])."""
+    c = cache.c
+    shape = (c.batch, c.heads_kv, k.shape[2], c.head_dim)
+    kr, vr = _rows(k, shape, k.dtype, "k"), _rows(v, shape, k.dtype, "v")
+    _check("vsa2_cache_write", vsa2_cache_write(c, _vdtype(k.dtype), shape[2], kr, vr,
+                                                _int_vector(start, c.batch, "start"),
+                                                _int_vector(count, c.batch, "count"), _stream()))
+
+
+def cache_read(cache, n, start, count=None, dtype=None, out=None):
+    """(k, v) [batch, heads_kv, n, D] of list positions start[b] .. start[b] + n - 1
+    (zeros past count[b] and where the list has no page); bf16 unless `dtype`
+    says float32.  `out` gives the two outputs (any strides)."""
+    torch = _torch()
+    c = cache.c
+    shape = (c.batch, c.heads_kv, n, c.head_dim)
+    if out is None:
+        dt = torch.bfloat16 if dtype is None else dtype
+        out = tuple(torch.empty(shape, dtype=dt, device=cache.pool.device) for _ in range(2))
+    k, v = out
+    kr, vr = _rows(k, shape, k.dtype, "k"), _rows(v, shape, k.dtype, "v")
+    _check("vsa2_cache_read", vsa2_cache_read(c, _vdtype(k.dtype), n, kr, vr, _int_vector(start, c.batch, "start"),
+                                              _int_vector(count, c.batch, "count"), _stream()))
+    return k, v
+
+
+def attn_cache(cache, q, length, count=None, causal=False, o=None):
+    """Attention of q [batch, heads_q, n, D] (any strides) over each sequence's
+    first length[b] list positions; causal: the call's tokens are the last
+    count[b] (None: n) of them and see no later one.  Returns (o, lse), o like q
+    and contiguous unless given, lse [batch, heads_q, n] fp32."""
+    torch = _torch()
+    c = cache.c
+    heads, n = q.shape[1], q.shape[2]
+    shape = (c.batch, heads, n, c.head_dim)
+    qr = _rows(q, shape, q.dtype, "q")
+    if o is None:
+        o = torch.empty(shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(shape[:3], dtype=torch.float32, device=q.device)
+    st, wsb = vsa2_attn_cache_workspace(c, heads, n)
+    _check("vsa2_attn_cache_workspace", st)
+    ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
+    _check("vsa2_attn_cache", vsa2_attn_cache(c, _vdtype(q.dtype), heads, n, qr,
+                                              _int_vector(length, c.batch, "length"),
+                                              _int_vector(count, c.batch, "count"), int(bool(causal)),
+                                              _rows(o, shape, q.dtype, "o"), lse.data_ptr(), _ptr(ws), wsb,
+                                              _stream()))
+    return o, lse

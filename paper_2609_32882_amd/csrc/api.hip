@@ -122,6 +122,117 @@ size_t bwd_ws_bytes(const shape& s, const vsa2_problem* p) {
         if ((expr) != hipSuccess) return VSA2_ERR_HIP; \
     } while (0)
 
+// Rows of a projection: pointer, alignment and strides of the axes that have
+// more than one entry.  Written rows must not share memory.
+vsa2_status check_rows(const vsa2_rows* r, int32_t dtype, int64_t batch, int64_t heads, int64_t tokens, bool written) {
+    if (!r || !r->ptr) return VSA2_ERR_NULL;
+    if (!aligned16(r->ptr)) return VSA2_ERR_ALIGN;
+    const int64_t per16 = dtype == VSA2_BF16 ? 8 : 4;
+    const int64_t stride[3] = {r->batch, r->head, r->token}, count[3] = {batch, heads, tokens};
+    for (int i = 0; i < 3; ++i) {
+        if (count[i] < 2) continue;
+        if (stride[i] < 0 || (written && stride[i] == 0)) return VSA2_ERR_SHAPE;
+        if (stride[i] % per16) return VSA2_ERR_ALIGN;
+    }
+    return VSA2_OK;
+}
+
+vsa2::row_view view_of(const vsa2_rows* r) {
+    return r ? vsa2::row_view{r->ptr, r->batch, r->head, r->token} : vsa2::row_view{nullptr, 0, 0, 0};
+}
+
+// What norm and rotation check in both directions; fills the kernel's arguments.
+vsa2_status rope_setup(const vsa2_problem* p, const vsa2_rope* r, float eps, const float* q_gain, const float* k_gain,
+                       shape* s, vsa2::rope_args* a) {
+    vsa2_status st = check_problem(p, s);
+    if (st != VSA2_OK) return st;
+    if (p->head_dim != 64 && p->head_dim != 128) return VSA2_ERR_UNSUPPORTED;
+    if (!(eps >= 0.f) || eps > 3.402823466e38f) return VSA2_ERR_VALUE;
+    if (eps == 0.f && (q_gain || k_gain)) return VSA2_ERR_VALUE;
+    *a = vsa2::rope_args{};
+    a->grid = grid_of(p);
+    a->Lj = s->Lj;
+    a->eps = eps;
+    if (s->Lj > ((int64_t(1) << 31) - 1) / p->batch) return VSA2_ERR_UNSUPPORTED;
+    a->tokens = p->batch * s->Lj;
+    a->part[0].gain = q_gain;
+    a->part[1].gain = k_gain;
+    if (!r) return VSA2_OK;
+    if (r->pairing != VSA2_ROPE_ADJACENT && r->pairing != VSA2_ROPE_HALVES) return VSA2_ERR_VALUE;
+    const int32_t grid[3] = {p->T, p->H, p->W};
+    int64_t sum = 0;
+    for (int x = 0; x < 3; ++x) {
+        if (r->axis[x] < 0 || r->axis[x] % 2) return VSA2_ERR_SHAPE;
+        if (!r->axis[x]) continue;
+        if (!r->table[x]) return VSA2_ERR_NULL;
+        if (reinterpret_cast<uintptr_t>(r->table[x]) % 8) return VSA2_ERR_ALIGN;
+        if (r->rows[x] < 1 || (!r->origin && r->rows[x] < grid[x])) return VSA2_ERR_SHAPE;
+        sum += r->axis[x];
+        a->axis_pairs[x] = r->axis[x] / 2;
+        a->table_rows[x] = r->rows[x];
+        a->table[x] = r->table[x];
+    }
+    if (sum > p->head_dim) return VSA2_ERR_SHAPE;
+    if (r->pairing == VSA2_ROPE_HALVES && sum % 8) return VSA2_ERR_SHAPE;
+    a->pairs = static_cast<int>(sum / 2);
+    a->origin = r->origin;
+    return VSA2_OK;
+}
+
+bool halves_of(const vsa2_rope* r) { return r && r->pairing == VSA2_ROPE_HALVES; }
+
+// The cache's own fields, its view for the kernels, and rows of the call's tokens.
+vsa2_status check_cache(const vsa2_cache* c, int32_t dtype, int32_t n, vsa2::cache_view* v) {
+    if (!c) return VSA2_ERR_NULL;
+    if (dtype != VSA2_F32 && dtype != VSA2_BF16) return VSA2_ERR_DTYPE;
+    if (c->batch < 1 || c->heads_kv < 1 || c->pages < 1 || c->max_pages < 1 || n < 0) return VSA2_ERR_SHAPE;
+    if (c->table_heads != 1 && c->table_heads != c->heads_kv) return VSA2_ERR_SHAPE;
+    if (c->head_dim != 64 && c->head_dim != 128) return VSA2_ERR_UNSUPPORTED;
+    // list positions are 32-bit inside the kernels, page addresses 64-bit
+    if (c->max_pages > (1 << 24)) return VSA2_ERR_UNSUPPORTED;
+    *v = vsa2::cache_view{static_cast<char*>(c->pool), c->table, c->batch, c->heads_kv, c->pages, c->max_pages,
+                          c->table_heads};
+    return VSA2_OK;
+}
+
+vsa2_status check_cache_memory(const vsa2_cache* c) {
+    if (!c->pool || !c->table) return VSA2_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(c->pool) % kAlign) return VSA2_ERR_ALIGN;
+    return VSA2_OK;
+}
+
+constexpr int64_t kMaxWorkgroups = (int64_t(1) << 31) - 1;
+
+vsa2_status cache_copy(bool write, const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k,
+                       const vsa2_rows* v, const int32_t* start, const int32_t* count, hipStream_t stream) {
+    vsa2::cache_view view;
+    vsa2_status st = check_cache(c, dtype, n, &view);
+    if (st != VSA2_OK) return st;
+    if (n == 0) return VSA2_OK;
+    if ((st = check_cache_memory(c)) != VSA2_OK) return st;
+    if (!start) return VSA2_ERR_NULL;
+    if ((st = check_rows(k, dtype, c->batch, c->heads_kv, n, !write)) != VSA2_OK) return st;
+    if ((st = check_rows(v, dtype, c->batch, c->heads_kv, n, !write)) != VSA2_OK) return st;
+    if (static_cast<int64_t>(c->batch) * c->heads_kv > kMaxWorkgroups / (n / 64 + 2)) return VSA2_ERR_UNSUPPORTED;
+    if (vsa2::launch_cache_copy(write, dtype, c->head_dim, view, n, view_of(k), view_of(v), start, count, stream) !=
+        hipSuccess)
+        return VSA2_ERR_HIP;
+    return VSA2_OK;
+}
+
+// What attention over the cache and its workspace query check alike.
+vsa2_status check_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n, vsa2::cache_view* view) {
+    const vsa2_status st = check_cache(c, dtype, n, view);
+    if (st != VSA2_OK) return st;
+    if (heads_q < 1 || heads_q % c->heads_kv) return VSA2_ERR_SHAPE;
+    // rows of a KV head, and workgroups of the unsplit launch
+    const int64_t group = heads_q / c->heads_kv;
+    if (group * n > (int64_t(1) << 30)) return VSA2_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(c->batch) * c->heads_kv > (int64_t(1) << 30) / (group * n / 16 + 1))
+        return VSA2_ERR_UNSUPPORTED;
+    return VSA2_OK;
+}
+
 // entries of the joint lists beyond the video ones: the text blocks of the
 // video rows and the full text rows
 int64_t joint_extra(const vsa2_problem* p, const shape& s) {
@@ -144,6 +255,7 @@ const char* vsa2_status_str(vsa2_status s) {
         case VSA2_ERR_WORKSPACE: return "workspace missing or too small";
         case VSA2_ERR_HIP: return "HIP launch failed";
         case VSA2_ERR_UNSUPPORTED: return "shape outside the supported kernel configurations";
+        case VSA2_ERR_VALUE: return "scalar argument outside its range";
     }
     return "unknown status";
 }
@@ -526,6 +638,128 @@ vsa2_status vsa2_unpool_add(const vsa2_problem* p, int32_t heads, const void* dx
     VSA2_TRY_HIP(vsa2::launch_unpool_add(p->dtype, p->head_dim, dx_c, dx,
                                          static_cast<int64_t>(p->batch) * heads * s.L, s.L, s.Lj,
                                          static_cast<int>(s.N), grid_of(p), Pt, Ph, Pw, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_qk_norm_rope(const vsa2_problem* p, const vsa2_rope* r, float eps, const vsa2_rows* q_in,
+                              const float* q_gain, void* q, const vsa2_rows* k_in, const float* k_gain, void* k,
+                              const vsa2_rows* v_in, void* v, hipStream_t stream) {
+    shape s;
+    vsa2::rope_args a;
+    vsa2_status st = rope_setup(p, r, eps, q_gain, k_gain, &s, &a);
+    if (st != VSA2_OK) return st;
+    const int64_t real = static_cast<int64_t>(p->T) * p->H * p->W + p->text_len;
+    const vsa2_rows* in[3] = {q_in, k_in, v_in};
+    void* out[3] = {q, k, v};
+    for (int x = 0; x < 3; ++x) {
+        if (!in[x] && !out[x]) continue;
+        const int heads = x ? p->heads_kv : p->heads_q;
+        if (!out[x]) return VSA2_ERR_NULL;
+        if ((st = check_rows(in[x], p->dtype, p->batch, heads, real, false)) != VSA2_OK) return st;
+        if (!aligned16(out[x])) return VSA2_ERR_ALIGN;
+        a.part[x].x = view_of(in[x]);
+        a.part[x].y = out[x];
+        a.part[x].heads = heads;
+    }
+    VSA2_TRY_HIP(vsa2::launch_norm_rope(p->dtype, p->head_dim, halves_of(r), a, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_qk_norm_rope_workspace(const vsa2_problem* p, size_t* bytes) {
+    shape s;
+    vsa2::rope_args a;
+    const vsa2_status st = rope_setup(p, nullptr, 0.f, nullptr, nullptr, &s, &a);
+    if (st != VSA2_OK) return st;
+    if (!bytes) return VSA2_ERR_NULL;
+    *bytes = align_up(vsa2::norm_rope_workspace_bytes(p->head_dim, a.tokens, p->heads_q + 2 * p->heads_kv));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_qk_norm_rope_bwd(const vsa2_problem* p, const vsa2_rope* r, float eps, const vsa2_rows* q_in,
+                                  const float* q_gain, const void* dq, const vsa2_rows* dq_in, float* dq_gain,
+                                  const vsa2_rows* k_in, const float* k_gain, const void* dk,
+                                  const vsa2_rows* dk_in, float* dk_gain, const void* dv, const vsa2_rows* dv_in,
+                                  void* ws, size_t ws_bytes, hipStream_t stream) {
+    shape s;
+    vsa2::rope_args a;
+    vsa2_status st = rope_setup(p, r, eps, q_gain, k_gain, &s, &a);
+    if (st != VSA2_OK) return st;
+    if (eps == 0.f && (dq_gain || dk_gain)) return VSA2_ERR_VALUE;
+    const int64_t real = static_cast<int64_t>(p->T) * p->H * p->W + p->text_len;
+    const vsa2_rows* in[3] = {q_in, k_in, nullptr};
+    const void* dy[3] = {dq, dk, dv};
+    const vsa2_rows* dx[3] = {dq_in, dk_in, dv_in};
+    float* dgain[2] = {dq_gain, dk_gain};
+    for (int x = 0; x < 3; ++x) {
+        if (!dy[x] && !dx[x]) {
+            if (x < 2 && dgain[x]) return VSA2_ERR_NULL;    // a gain's gradient needs its rows
+            continue;
+        }
+        const int heads = x ? p->heads_kv : p->heads_q;
+        if (!dy[x]) return VSA2_ERR_NULL;
+        if (!aligned16(dy[x])) return VSA2_ERR_ALIGN;
+        if ((st = check_rows(dx[x], p->dtype, p->batch, heads, real, true)) != VSA2_OK) return st;
+        if (x < 2 && eps > 0.f) {
+            if ((st = check_rows(in[x], p->dtype, p->batch, heads, real, false)) != VSA2_OK) return st;
+            a.part[x].x = view_of(in[x]);
+        }
+        a.part[x].dx = view_of(dx[x]);
+        a.part[x].y = const_cast<void*>(dy[x]);
+        a.part[x].heads = heads;
+    }
+    if (dq_gain || dk_gain) {
+        const size_t need =
+            align_up(vsa2::norm_rope_workspace_bytes(p->head_dim, a.tokens, p->heads_q + 2 * p->heads_kv));
+        if (!ws || ws_bytes < need) return VSA2_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
+        a.partial = static_cast<float*>(ws);
+    }
+    VSA2_TRY_HIP(vsa2::launch_norm_rope_bwd(p->dtype, p->head_dim, halves_of(r), a, dq_gain, dk_gain, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_cache_page_bytes(int32_t head_dim, size_t* bytes) {
+    if (!bytes) return VSA2_ERR_NULL;
+    if (head_dim != 64 && head_dim != 128) return VSA2_ERR_UNSUPPORTED;
+    *bytes = static_cast<size_t>(vsa2::cache_page_bytes(head_dim));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_cache_write(const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k, const vsa2_rows* v,
+                             const int32_t* start, const int32_t* count, hipStream_t stream) {
+    return cache_copy(true, c, dtype, n, k, v, start, count, stream);
+}
+
+vsa2_status vsa2_cache_read(const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k, const vsa2_rows* v,
+                            const int32_t* start, const int32_t* count, hipStream_t stream) {
+    return cache_copy(false, c, dtype, n, k, v, start, count, stream);
+}
+
+vsa2_status vsa2_attn_cache_workspace(const vsa2_cache* c, int32_t heads_q, int32_t n, size_t* bytes) {
+    vsa2::cache_view view;
+    const vsa2_status st = check_attn_cache(c, VSA2_F32, heads_q, n, &view);
+    if (st != VSA2_OK) return st;
+    if (!bytes) return VSA2_ERR_NULL;
+    *bytes = n == 0 ? 0 : align_up(vsa2::attn_cache_workspace_bytes(view, c->head_dim, heads_q, n));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n, const vsa2_rows* q,
+                            const int32_t* length, const int32_t* count, int32_t causal, const vsa2_rows* o,
+                            float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+    vsa2::cache_view view;
+    vsa2_status st = check_attn_cache(c, dtype, heads_q, n, &view);
+    if (st != VSA2_OK) return st;
+    if (n == 0) return VSA2_OK;
+    if ((st = check_cache_memory(c)) != VSA2_OK) return st;
+    if (!length || !lse) return VSA2_ERR_NULL;
+    if ((st = check_rows(q, dtype, c->batch, heads_q, n, false)) != VSA2_OK) return st;
+    if ((st = check_rows(o, dtype, c->batch, heads_q, n, true)) != VSA2_OK) return st;
+    const size_t need = align_up(vsa2::attn_cache_workspace_bytes(view, c->head_dim, heads_q, n));
+    if (need && (!ws || ws_bytes < need)) return VSA2_ERR_WORKSPACE;
+    if (need && reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
+    VSA2_TRY_HIP(vsa2::launch_attn_cache(dtype, c->head_dim, view, heads_q, n, view_of(q), length, count, causal != 0,
+                                         view_of(o), lse, ws, stream));
     return VSA2_OK;
 }
 

@@ -1,0 +1,420 @@
+// Attention of new tokens over the paged 8-bit cache.
+//
+// Rows: the query heads of one KV head times the call's tokens (token-major), in
+// tiles of 16.  Everything is computed transposed, S^T = K Q^T and
+// O^T = V^T P^T on 16x16x32 bf16 MFMAs, so that a lane holds one row (column
+// lane % 16) through the whole kernel: the softmax needs two exchanges a page,
+// P goes from the accumulators of the first product into the operand of the
+// second without leaving its lane (the page's V order is made for that), and O
+// is rescaled lane by lane.  e4m3 codes become bf16 exactly: K's with the
+// token's power applied by the conversion, V's plain, with the power on P.
+// fp32 queries and probabilities are three bf16 terms each, so their products
+// lose nothing that fp32 sums would keep.
+//
+// Bound by memory for single tokens: 2 (D + 1) bytes per token and KV head.  A
+// page is 16 KB in runs of 1 KB per load instruction; the waves of a workgroup
+// and the workgroups of a split take different pages of a list, each with its
+// own running maximum and sum, and are joined at the end in a fixed order.
+#include "common.hpp"
+
+namespace vsa2 {
+
+namespace {
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+
+constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896340f;
+constexpr int TILE = 16;          // rows of a workgroup
+constexpr int NW = 4;             // waves of a workgroup
+
+struct attn_args {
+    cache_view c;
+    row_view q, o;
+    float* lse;
+    const int32_t* length;
+    const int32_t* count;
+    float* part;         // [items][splits]: O [16][D], then (m, l) [16][2] of each
+    int n, group, rows, tiles, splits;
+    bool causal;
+};
+
+template <typename T> constexpr int terms_of = sizeof(T) == 4 ? 3 : 1;
+
+// 8 values as the sum of bf16 fragments (one, or three for fp32: 24 bits).
+template <int N>
+__device__ __forceinline__ void split_frag(frag_bf16* f, const float* x) {
+    if constexpr (N == 1) {
+        pack_frag(f[0], x);
+    } else {
+        float rest[8];
+        frag_bf16 cut;
+        pack_frag_hilo(f[0], cut, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] = x[i] - static_cast<float>(f[0].v[i]);
+        pack_frag_hilo(f[1], f[2], rest);
+    }
+}
+
+// 8 e4m3 codes times a power of two, in bf16 (exact).
+__device__ __forceinline__ frag_bf16 decode8(uint32_t a, uint32_t b, float power) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+    u32x4_t w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(a), power, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(a), power, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(b), power, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(b), power, true));
+    frag_bf16 f;
+    f.v = __builtin_bit_cast(bf16x8_t, w);
+    return f;
+}
+
+__device__ __forceinline__ f32x4_t mma16(const frag_bf16& a, const frag_bf16& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+__device__ __forceinline__ void store4(float* p, const float* x) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void store4(bf16_t* p, const float* x) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]));
+}
+
+__device__ __forceinline__ int lanes_max(int x) {       // over the 16 rows of a tile
+#pragma unroll
+    for (int m = 8; m; m >>= 1) x = max(x, __shfl_xor(x, m, 64));
+    return x;
+}
+__device__ __forceinline__ int lanes_min(int x) {
+#pragma unroll
+    for (int m = 8; m; m >>= 1) x = min(x, __shfl_xor(x, m, 64));
+    return x;
+}
+
+// What row r of sequence b sees: list positions below this.
+__device__ __forceinline__ int row_limit(const attn_args& a, int b, int r) {
+    if (r >= a.rows) return 0;
+    const int i = r / a.group;
+    int cnt = a.n;
+    if (a.count) cnt = min(max(a.count[b], 0), a.n);
+    if (i >= cnt) return 0;
+    const int64_t most = static_cast<int64_t>(a.c.max_pages) * CACHE_TOKENS;
+    int64_t len = a.length[b];
+    len = len < 0 ? 0 : (len > most ? most : len);
+    if (a.causal) len -= cnt - 1 - i;
+    return static_cast<int>(len < 0 ? 0 : len);
+}
+
+// One row tile's state in one wave: its running maximum and sum (base 2) and
+// O^T, rows d = 16 c + 4 g + i, column lane % 16.
+template <int D>
+struct tile_state {
+    float m, l;
+    f32x4_t o[D / 16];
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void page_step(const char* page, int64_t pos, int limit, int lim_min, int lim_max,
+                                          const frag_bf16 (&qf)[D / 32][terms_of<T>], float scale,
+                                          tile_state<D>& st) {
+    constexpr int NT = terms_of<T>;
+    const int lane = lane_id(), g = lane >> 4;
+    const uint4* kp = reinterpret_cast<const uint4*>(page) + lane;
+    const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
+    uint4 kr[4 * (D / 64)], vr[D / 16];
+#pragma unroll
+    for (int i = 0; i < 4 * (D / 64); ++i) kr[i] = kp[i * 64];
+    const uint32_t ke = *reinterpret_cast<const uint32_t*>(page + 128 * D + (lane & 15) * 4);
+    const uint4 ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + g * 16);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) vr[i] = vp[i * 64];
+
+    f32x4_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const float power = power_of((ke >> (8 * t)) & 0xffu);
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u) {
+            const uint4 w = kr[t * (D / 64) + u];
+            const frag_bf16 k0 = decode8(w.x, w.y, power), k1 = decode8(w.z, w.w, power);
+#pragma unroll
+            for (int x = NT - 1; x >= 0; --x) {
+                s[t] = mma16(k0, qf[2 * u][x], s[t]);
+                s[t] = mma16(k1, qf[2 * u + 1][x], s[t]);
+            }
+        }
+    }
+    const uint32_t vw[4] = {ve.x, ve.y, ve.z, ve.w};
+    const bool masked = pos + CACHE_TOKENS > lim_min;
+    float p[4][4], mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = s[t][i] * scale;
+            if (masked && pos + 16 * t + 4 * g + i >= limit) x = -INFINITY;
+            p[t][i] = x;
+            mx = fmaxf(mx, x);
+        }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m = fmaxf(st.m, mx), base = m == -INFINITY ? 0.f : m;
+    const float alpha = fast_exp2(st.m - base);
+    st.m = m;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float e = fast_exp2(p[t][i] - base);
+            sum += e;
+            // a masked place's power may be anything
+            p[t][i] = masked && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
+        }
+    st.l = st.l * alpha + sum;
+    frag_bf16 pf[2][NT];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const float y[8] = {p[2 * x][0], p[2 * x][1], p[2 * x][2], p[2 * x][3],
+                            p[2 * x + 1][0], p[2 * x + 1][1], p[2 * x + 1][2], p[2 * x + 1][3]};
+        split_frag<NT>(pf[x], y);
+    }
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) st.o[c] *= alpha;
+    if (masked) {
+        // Codes past every row's limit are whatever the page held: taken as
+        // zeros.  A NaN below it, which some rows see and others do not, is
+        // taken out of the product and given to the rows that see it (a second
+        // product counts their weight on it).
+        uint32_t keep[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t left = lim_max - (pos + 16 * t + 4 * g);
+            keep[t] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * static_cast<int>(left)));
+        }
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t w[4] = {vr[c].x & keep[0], vr[c].y & keep[1], vr[c].z & keep[2], vr[c].w & keep[3]}, nan[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                nan[t] = ((((w[t] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+                w[t] &= ~nan[t];
+            }
+            vr[c] = make_uint4(w[0], w[1], w[2], w[3]);
+            if (__ballot((nan[0] | nan[1] | nan[2] | nan[3]) != 0) != 0) {
+                f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                const uint32_t one = 0x38383838u;      // 1.0 in e4m3
+                hit = mma16(decode8(nan[0] & one, nan[1] & one, 1.f), pf[0][0], hit);
+                hit = mma16(decode8(nan[2] & one, nan[3] & one, 1.f), pf[1][0], hit);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+        const frag_bf16 v0 = decode8(vr[c].x, vr[c].y, 1.f), v1 = decode8(vr[c].z, vr[c].w, 1.f);
+#pragma unroll
+        for (int x = NT - 1; x >= 0; --x) {
+            st.o[c] = mma16(v0, pf[0][x], st.o[c]);
+            st.o[c] = mma16(v1, pf[1][x], st.o[c]);
+        }
+    }
+}
+
+// Element offset of row r (query head and token of KV head h) in q or o.
+__device__ __forceinline__ int64_t row_offset(const row_view& v, const attn_args& a, int b, int h, int r) {
+    const int i = r / a.group, hg = r - i * a.group;
+    return b * v.batch + static_cast<int64_t>(h * a.group + hg) * v.head + static_cast<int64_t>(i) * v.token;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
+    constexpr int NT = terms_of<T>;
+    __shared__ float so[NW][TILE][D + 4];
+    __shared__ float sml[NW][TILE][2];
+    const int lane = lane_id(), wave = wave_id(), g = lane >> 4, col = lane & 15;
+    // row tiles of a list's piece share its pages: next to each other on one XCD
+    uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
+    const int tile = static_cast<int>(item % a.tiles);
+    item /= a.tiles;
+    const int split = static_cast<int>(item % a.splits);
+    const uint32_t bh = item / a.splits;
+    const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
+    const int r = tile * TILE + col;
+    const int limit = row_limit(a, b, r);
+    const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(limit));
+    const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(limit));
+    const int pages = (lim_max + CACHE_TOKENS - 1) / CACHE_TOKENS;
+    const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
+    const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
+
+    frag_bf16 qf[D / 32][NT];
+    const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) {
+        float y[8] = {};
+        if (r < a.rows) {
+            const T* e = q + (x / 2) * 64 + g * 16 + (x & 1) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
+        }
+        split_frag<NT>(qf[x], y);
+    }
+    tile_state<D> st;
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) st.o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const float scale = LOG2E / sqrtf(static_cast<float>(D));
+    const int32_t* table =
+        a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
+    for (int pg = lo + wave; pg < hi; pg += NW) {
+        const int id = __builtin_amdgcn_readfirstlane(table[pg]);
+        if (id < 0 || id >= a.c.pages) continue;
+        const char* page = a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D);
+        page_step<T, D>(page, static_cast<int64_t>(pg) * CACHE_TOKENS, limit, lim_min, lim_max, qf, scale, st);
+    }
+    st.l += __shfl_xor(st.l, 16, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) so[wave][col][16 * c + 4 * g + i] = st.o[c][i];
+    if (g == 0) {
+        sml[wave][col][0] = st.m;
+        sml[wave][col][1] = st.l;
+    }
+    __syncthreads();
+    // join the waves: thread (row, D/16 elements)
+    const int row = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16);
+    float m = sml[0][row][0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, sml[w][row][0]);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[D / 16] = {};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const float f = fast_exp2(sml[w][row][0] - base);
+        l += f * sml[w][row][1];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] += f * so[w][row][d0 + i];
+    }
+    const int rr = tile * TILE + row;
+    if (a.splits > 1) {
+        float* part = a.part + ((static_cast<int64_t>(bh) * a.tiles + tile) * a.splits + split) * (TILE * (D + 2));
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4) store4(part + row * D + d0 + i, o + i);
+        if (threadIdx.x % 16 == 0) {
+            part[TILE * D + 2 * row] = m;
+            part[TILE * D + 2 * row + 1] = l;
+        }
+        return;
+    }
+    if (rr >= a.rows) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + d0;
+#pragma unroll
+    for (int i = 0; i < D / 16; i += 4) store4(out + i, o + i);
+    if (threadIdx.x % 16 == 0) {
+        const int i = rr / a.group, hg = rr - i * a.group;
+        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
+    }
+}
+
+// Joins the splits of a row tile, in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a) {
+    const uint32_t item = blockIdx.x, bh = item / a.tiles;
+    const int tile = static_cast<int>(item % a.tiles);
+    const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
+    const int row = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), rr = tile * TILE + row;
+    if (rr >= a.rows) return;
+    const float* part = a.part + static_cast<int64_t>(item) * a.splits * (TILE * (D + 2));
+    float m = -INFINITY;
+    for (int x = 0; x < a.splits; ++x) m = fmaxf(m, part[x * TILE * (D + 2) + TILE * D + 2 * row]);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[D / 16] = {};
+    for (int x = 0; x < a.splits; ++x) {
+        const float* px = part + static_cast<int64_t>(x) * TILE * (D + 2);
+        const float f = fast_exp2(px[TILE * D + 2 * row] - base);
+        l += f * px[TILE * D + 2 * row + 1];
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4) {
+            const float4 y = *reinterpret_cast<const float4*>(px + row * D + d0 + i);
+            o[i] += f * y.x;
+            o[i + 1] += f * y.y;
+            o[i + 2] += f * y.z;
+            o[i + 3] += f * y.w;
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + d0;
+#pragma unroll
+    for (int i = 0; i < D / 16; i += 4) store4(out + i, o + i);
+    if (threadIdx.x % 16 == 0) {
+        const int i = rr / a.group, hg = rr - i * a.group;
+        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
+    }
+}
+
+// Pieces a list is split into: enough workgroups for the chip, a page for every
+// wave at least.
+int split_count(const cache_view& c, int64_t tiles) {
+    const int64_t items = static_cast<int64_t>(c.batch) * c.heads * tiles;
+    const int64_t want = (1024 + items - 1) / items, most = (c.max_pages + NW - 1) / NW;
+    return static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+}
+
+int64_t tiles_of(int heads_q, int heads, int n) {
+    return (static_cast<int64_t>(heads_q / heads) * n + TILE - 1) / TILE;
+}
+
+}  // namespace
+
+size_t attn_cache_workspace_bytes(const cache_view& c, int D, int heads_q, int n) {
+    const int64_t tiles = tiles_of(heads_q, c.heads, n);
+    const int splits = split_count(c, tiles);
+    if (splits == 1) return 0;
+    return static_cast<size_t>(c.batch) * c.heads * tiles * splits * TILE * (D + 2) * sizeof(float);
+}
+
+hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
+                             const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
+                             void* ws, hipStream_t s) {
+    attn_args a{};
+    a.c = c;
+    a.q = q;
+    a.o = o;
+    a.lse = lse;
+    a.length = length;
+    a.count = count;
+    a.part = static_cast<float*>(ws);
+    a.n = n;
+    a.group = heads_q / c.heads;
+    a.rows = a.group * n;
+    a.tiles = static_cast<int>(tiles_of(heads_q, c.heads, n));
+    a.splits = split_count(c, a.tiles);
+    a.causal = causal;
+    const unsigned items = static_cast<unsigned>(static_cast<int64_t>(c.batch) * c.heads * a.tiles);
+#define VSA2_ATTN_GO(T, DD)                                                                                      \
+    do {                                                                                                         \
+        hipLaunchKernelGGL((attn_cache_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);          \
+        if (a.splits > 1) hipLaunchKernelGGL((attn_cache_join_kernel<T, DD>), dim3(items), dim3(256), 0, s, a);  \
+    } while (0)
+    if (dtype == 0 && D == 64) VSA2_ATTN_GO(float, 64);
+    else if (dtype == 0) VSA2_ATTN_GO(float, 128);
+    else if (D == 64) VSA2_ATTN_GO(bf16_t, 64);
+    else VSA2_ATTN_GO(bf16_t, 128);
+#undef VSA2_ATTN_GO
+    return hipGetLastError();
+}
+
+}  // namespace vsa2

@@ -186,4 +186,50 @@ hipError_t launch_attn_bwd_dq(int dtype, int D, const void* q, const void* k, co
                               void* dq, void* ws, int batch, int Hq, int Hkv, int N, const cube_grid& cg,
                               hipStream_t s);
 
+// Norm, rotation and cube-major layout of q, k, v (rope.hip).  Strides in
+// elements; a part without heads is left out.
+struct row_view {
+    void* ptr;
+    int64_t batch, head, token;
+};
+struct rope_part {
+    row_view x;         // the projection's rows (the gradients': read for the norm)
+    row_view dx;        // gradients: the rows written
+    const float* gain;   // null for ones
+    void* y;             // cube-major rows: written forward, read (dy) backward
+    int heads;
+};
+struct rope_args {
+    rope_part part[3];   // q, k, v
+    cube_grid grid;
+    int64_t Lj;          // cube-major places of a sequence
+    int64_t tokens;      // batch * Lj, below 2^31
+    float eps;           // 0: no norm
+    int pairs;           // turned pairs of a head
+    int axis_pairs[3], table_rows[3];
+    const float* table[3];
+    const int32_t* origin;
+    float* partial;      // gradients: the gains' partial rows, or null
+};
+hipError_t launch_norm_rope(int dtype, int D, bool halves, const rope_args& a, hipStream_t s);
+size_t norm_rope_workspace_bytes(int D, int64_t tokens, int heads);
+hipError_t launch_norm_rope_bwd(int dtype, int D, bool halves, const rope_args& a, float* dq_gain, float* dk_gain,
+                                hipStream_t s);
+
+// The paged 8-bit cache (cache.hip) and attention over it (attn_cache.hip).
+constexpr int CACHE_TOKENS = 64;   // tokens of a page
+__host__ __device__ constexpr int64_t cache_page_bytes(int D) { return 128 * static_cast<int64_t>(D) + 128; }
+struct cache_view {
+    char* pool;
+    const int32_t* table;
+    int batch, heads, pages, max_pages, table_heads;
+};
+// write: rows -> pages, else pages -> rows.
+hipError_t launch_cache_copy(bool write, int dtype, int D, const cache_view& c, int n, const row_view& k,
+                             const row_view& v, const int32_t* start, const int32_t* count, hipStream_t s);
+size_t attn_cache_workspace_bytes(const cache_view& c, int D, int heads_q, int n);
+hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
+                             const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
+                             void* ws, hipStream_t s);
+
 }  // namespace vsa2

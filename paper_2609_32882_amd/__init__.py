@@ -320,13 +320,23 @@ def select_from(obj) -> vsa2_select:
     return vsa2_select(int(obj.mode), int(obj.k), float(obj.mass), int(obj.cap))
 
 
+_TORCH = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
 
 
 def _stream():
-    return _torch().cuda.current_stream().cuda_stream
+    """torch's current stream as a hipStream_t.  The Stream object that
+    torch.cuda.current_stream() makes costs 3.5 us, a third of a small call's
+    host time; the raw handle is read in 0.2 us."""
+    c = _torch()._C
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _ptr(t):
@@ -583,25 +593,19 @@ def unpool_add(p, dx_c, dx, P):
 
 def _rows(t, shape, dtype, name):
     """vsa2_rows of t [batch, heads, tokens, D] with any strides but D's."""
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.stride(3) != 1:
+    stride = t.stride()
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or stride[3] != 1:
         raise ValueError("%s: expected %s %s on the GPU with contiguous rows, got %s %s strides %s" %
-                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape), tuple(t.stride())))
-    b, h, n, _ = t.stride()
-    return vsa2_rows(t.data_ptr(), b, h, n)
+                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape), tuple(stride)))
+    return vsa2_rows(t.data_ptr(), stride[0], stride[1], stride[2])
 
 
-def _int_vector(t, n, name):
-    """Pointer of an int32 GPU vector [n], or None."""
+def _vector(t, shape, dtype, name):
+    """Pointer of a contiguous GPU tensor of that shape and dtype, or None."""
     if t is None:
         return None
-    _expect(t, (n,) if isinstance(n, int) else n, _torch().int32, name)
-    return t.data_ptr()
-
-
-def _gain(t, D, name):
-    if t is None:
-        return None
-    _expect(t, (D,), _torch().float32, name)
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        _expect(t, shape, dtype, name)
     return t.data_ptr()
 
 
@@ -629,63 +633,54 @@ class Rope:
     [batch, 3] position of each sequence's first token (None: the grid's own),
     and which elements pair up ("adjacent" or "halves")."""
 
-    __slots__ = ("c", "keep")
+    __slots__ = ("c", "tables", "origin")
+    PAIRINGS = {"adjacent": VSA2_ROPE_ADJACENT, "halves": VSA2_ROPE_HALVES}
 
     def __init__(self, axes, tables, origin=None, pairing="adjacent"):
         torch = _torch()
-        c = vsa2_rope(pairing={"adjacent": VSA2_ROPE_ADJACENT, "halves": VSA2_ROPE_HALVES}[pairing])
-        for i, (n, t) in enumerate(zip(axes, tables)):
-            c.axis[i] = n
+        pairs = self.PAIRINGS[pairing]
+        rows, ptrs = [0, 0, 0], [None, None, None]
+        for i, n in enumerate(axes):
             if n:
-                _expect(t, (t.shape[0], n // 2, 2), torch.float32, "tables[%d]" % i)
-                c.rows[i], c.table[i] = t.shape[0], t.data_ptr()
-        if origin is not None:
-            _expect(origin, (origin.shape[0], 3), torch.int32, "origin")
-            c.origin = origin.data_ptr()
-        self.c, self.keep = c, (tables, origin)
-
-    def check(self, p):
-        origin = self.keep[1]
-        if origin is not None and origin.shape[0] != p.batch:
-            raise ValueError("origin: expected %d sequences, got %d" % (p.batch, origin.shape[0]))
-        return self.c
+                t = tables[i]
+                if t is None:
+                    raise ValueError("tables[%d]: an axis of %d elements needs one" % (i, n))
+                rows[i] = t.shape[0]
+                ptrs[i] = _vector(t, (rows[i], n // 2, 2), torch.float32, "tables")
+        at = None if origin is None else _vector(origin, (origin.shape[0], 3), torch.int32, "origin")
+        self.c = vsa2_rope(tuple(axes), tuple(rows), tuple(ptrs), at, pairs)
+        self.tables, self.origin = tables, origin       # kept alive with their addresses
 
 
-def _rope_c(rope, p):
-    return None if rope is None else rope.check(p)
-
-
-def _raster(p):
-    """Tokens of a sequence before the cube-major layout: the grid, then the text."""
-    return p.T * p.H * p.W + p.text_len
+def _rope_ref(rope, p):
+    if rope is None:
+        return None
+    if rope.origin is not None and rope.origin.shape[0] != p.batch:
+        raise ValueError("origin: expected %d sequences, got %d" % (p.batch, rope.origin.shape[0]))
+    return ctypes.byref(rope.c)
 
 
 def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None, eps=0.0, out=None):
     """Per-head RMS norm (eps > 0) of q and k with their gains, rotation, and the
     cube-major layout of all three: q [batch, heads_q, tokens, D], k and v
-    [batch, heads_kv, tokens, D] in raster order (views of a fused projection
-    are fine), each may be None.  Returns (q, k, v) contiguous; `out` gives the
-    three outputs."""
+    [batch, heads_kv, tokens, D] in raster order, the grid and then the text
+    (views of a fused projection are fine); each may be None.  Returns (q, k, v)
+    contiguous; `out` gives the three outputs."""
     torch = _torch()
     p = problem_from(p)
-    dt, n, L, D = _tdtype(p), _raster(p), _joint(p)[1], p.head_dim
-    rows, ptrs, outs = [], [], []
-    for i, (x, name) in enumerate(((q, "q"), (k, "k"), (v, "v"))):
+    dt, batch, D, L = _tdtype(p), p.batch, p.head_dim, _joint(p)[1]
+    n = p.T * p.H * p.W + p.text_len
+    rows, ptrs, outs = [None] * 3, [None] * 3, [None] * 3
+    for i, x in enumerate((q, k, v)):
         if x is None:
-            rows.append(None), ptrs.append(None), outs.append(None)
             continue
         heads = p.heads_kv if i else p.heads_q
-        rows.append(_rows(x, (p.batch, heads, n, D), dt, name))
-        if out is not None:
-            y = out[i]
-            _expect(y, (p.batch, heads, L, D), dt, "out[%d]" % i)
-        else:
-            y = torch.empty((p.batch, heads, L, D), dtype=dt, device=x.device)
-        outs.append(y)
-        ptrs.append(y.data_ptr())
-    _check("vsa2_qk_norm_rope", vsa2_qk_norm_rope(p, _rope_c(rope, p), eps, rows[0], _gain(q_gain, D, "q_gain"),
-                                                  ptrs[0], rows[1], _gain(k_gain, D, "k_gain"), ptrs[1], rows[2],
-                                                  ptrs[2], _stream()))
+        rows[i] = ctypes.byref(_rows(x, (batch, heads, n, D), dt, "qkv"[i]))
+        y = outs[i] = x.new_empty((batch, heads, L, D)) if out is None else out[i]
+        ptrs[i] = _vector(y, (batch, heads, L, D), dt, "out")
+    _check("vsa2_qk_norm_rope", _lib().vsa2_qk_norm_rope(
+        ctypes.byref(p), _rope_ref(rope, p), eps, rows[0], _vector(q_gain, (D,), torch.float32, "q_gain"), ptrs[0],
+        rows[1], _vector(k_gain, (D,), torch.float32, "k_gain"), ptrs[1], rows[2], ptrs[2], _stream()))
     return tuple(outs)
 
 
@@ -698,30 +693,31 @@ def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, 
     norm; the gains' gradients come with them."""
     torch = _torch()
     p = problem_from(p)
-    dt, n, L, D = _tdtype(p), _raster(p), _joint(p)[1], p.head_dim
-    norm = eps > 0
-    dy, dx, dx_rows, x_rows, dgain = [], [], [], [], []
-    for i, (g, x, name) in enumerate(((dq, q, "q"), (dk, k, "k"), (dv, None, "v"))):
+    dt, batch, D, L = _tdtype(p), p.batch, p.head_dim, _joint(p)[1]
+    n = p.T * p.H * p.W + p.text_len
+    dy, x_rows, dx_rows, dx = [None] * 3, [None] * 3, [None] * 3, [None] * 3
+    for i, (g, x) in enumerate(((dq, q), (dk, k), (dv, None))):
         if g is None:
-            dy.append(None), dx.append(None), dx_rows.append(None), x_rows.append(None), dgain.append(None)
             continue
         heads = p.heads_kv if i else p.heads_q
-        _expect(g, (p.batch, heads, L, D), dt, "d" + name)
-        y = out[i] if out is not None else torch.empty((p.batch, n, heads, D), dtype=dt, device=g.device).transpose(1, 2)
-        dy.append(g.data_ptr())
-        dx.append(y)
-        dx_rows.append(_rows(y, (p.batch, heads, n, D), dt, "out[%d]" % i))
-        x_rows.append(_rows(x, (p.batch, heads, n, D), dt, name) if x is not None else None)
-        dgain.append(torch.empty(D, dtype=torch.float32, device=g.device) if norm and i < 2 else None)
-    wsb, ws = 0, None
-    if dgain[0] is not None or dgain[1] is not None:
+        shape = (batch, heads, n, D)
+        dy[i] = _vector(g, (batch, heads, L, D), dt, ("dq", "dk", "dv")[i])
+        dx[i] = g.new_empty((batch, n, heads, D)).transpose(1, 2) if out is None else out[i]
+        dx_rows[i] = ctypes.byref(_rows(dx[i], shape, dt, "out"))
+        if x is not None:
+            x_rows[i] = ctypes.byref(_rows(x, shape, dt, "qk"[i]))
+    dgain, ws, wsb = [None, None], None, 0
+    if eps > 0 and (dq is not None or dk is not None):
+        dev = (dq if dq is not None else dk).device
+        both = torch.empty((2, D), dtype=torch.float32, device=dev)
+        dgain = [both[0] if dq is not None else None, both[1] if dk is not None else None]
         st, wsb = vsa2_qk_norm_rope_workspace(p)
         _check("vsa2_qk_norm_rope_workspace", st)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=(dx[0] if dx[0] is not None else dx[1]).device)
-    _check("vsa2_qk_norm_rope_bwd", vsa2_qk_norm_rope_bwd(
-        p, _rope_c(rope, p), eps, x_rows[0], _gain(q_gain, D, "q_gain"), dy[0], dx_rows[0], _ptr(dgain[0]),
-        x_rows[1], _gain(k_gain, D, "k_gain"), dy[1], dx_rows[1], _ptr(dgain[1]), dy[2], dx_rows[2], _ptr(ws), wsb,
-        _stream()))
+        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
+    _check("vsa2_qk_norm_rope_bwd", _lib().vsa2_qk_norm_rope_bwd(
+        ctypes.byref(p), _rope_ref(rope, p), eps, x_rows[0], _vector(q_gain, (D,), torch.float32, "q_gain"), dy[0],
+        dx_rows[0], _ptr(dgain[0]), x_rows[1], _vector(k_gain, (D,), torch.float32, "k_gain"), dy[1], dx_rows[1],
+        _ptr(dgain[1]), dy[2], dx_rows[2], _ptr(ws), wsb, _stream()))
     return dx[0], dx[1], dx[2], dgain[0], dgain[1]
 
 
@@ -734,20 +730,15 @@ class KVCache:
 
     def __init__(self, pool, table):
         torch = _torch()
-        if pool.dim() != 3 or (pool.shape[2] - 128) % 128:
-            raise ValueError("pool: expected [pages, heads_kv, 128*D + 128], got %s" % (tuple(pool.shape),))
-        _expect(pool, pool.shape, torch.uint8, "pool")
-        _expect(table, table.shape, torch.int32, "table")
-        pages, heads = pool.shape[0], pool.shape[1]
-        if table.dim() == 2:
-            per_head = 1
-        elif table.dim() == 3 and table.shape[1] == heads:
-            per_head = heads
-        else:
+        shape, lists = pool.shape, table.shape
+        if len(shape) != 3 or shape[2] < 256 or (shape[2] - 128) % 128:
+            raise ValueError("pool: expected [pages, heads_kv, 128*D + 128], got %s" % (tuple(shape),))
+        if len(lists) != 2 and (len(lists) != 3 or lists[1] != shape[1]):
             raise ValueError("table: expected [batch, max_pages] or [batch, %d, max_pages], got %s" %
-                             (heads, tuple(table.shape)))
-        self.c = vsa2_cache(table.shape[0], heads, (pool.shape[2] - 128) // 128, pages, table.shape[-1], per_head,
-                            pool.data_ptr(), table.data_ptr())
+                             (shape[1], tuple(lists)))
+        self.c = vsa2_cache(lists[0], shape[1], (shape[2] - 128) // 128, shape[0], lists[-1],
+                            1 if len(lists) == 2 else lists[1], _vector(pool, shape, torch.uint8, "pool"),
+                            _vector(table, lists, torch.int32, "table"))
         self.pool, self.table = pool, table
 
     @classmethod
@@ -762,28 +753,32 @@ def cache_write(cache, k, v, start, count=None):
     """Quantise tokens k, v [batch, heads_kv, n, D] (any strides) into the cache:
     token i < count[b] (int32 [batch], None: all n) goes to list position
     start[b] + i (int32 [batch])."""
-    c = cache.c
-    shape = (c.batch, c.heads_kv, k.shape[2], c.head_dim)
-    kr, vr = _rows(k, shape, k.dtype, "k"), _rows(v, shape, k.dtype, "v")
-    _check("vsa2_cache_write", vsa2_cache_write(c, _vdtype(k.dtype), shape[2], kr, vr,
-                                                _int_vector(start, c.batch, "start"),
-                                                _int_vector(count, c.batch, "count"), _stream()))
+    i32, c = _torch().int32, cache.c
+    batch, dt = c.batch, k.dtype
+    shape = (batch, c.heads_kv, k.shape[2], c.head_dim)
+    _check("vsa2_cache_write", _lib().vsa2_cache_write(
+        ctypes.byref(c), _vdtype(dt), shape[2], ctypes.byref(_rows(k, shape, dt, "k")),
+        ctypes.byref(_rows(v, shape, dt, "v")), _vector(start, (batch,), i32, "start"),
+        _vector(count, (batch,), i32, "count"), _stream()))
 
 
 def cache_read(cache, n, start, count=None, dtype=None, out=None):
     """(k, v) [batch, heads_kv, n, D] of list positions start[b] .. start[b] + n - 1
     (zeros past count[b] and where the list has no page); bf16 unless `dtype`
     says float32.  `out` gives the two outputs (any strides)."""
-    torch = _torch()
-    c = cache.c
-    shape = (c.batch, c.heads_kv, n, c.head_dim)
+    torch, c = _torch(), cache.c
+    batch = c.batch
+    shape = (batch, c.heads_kv, n, c.head_dim)
     if out is None:
-        dt = torch.bfloat16 if dtype is None else dtype
-        out = tuple(torch.empty(shape, dtype=dt, device=cache.pool.device) for _ in range(2))
-    k, v = out
-    kr, vr = _rows(k, shape, k.dtype, "k"), _rows(v, shape, k.dtype, "v")
-    _check("vsa2_cache_read", vsa2_cache_read(c, _vdtype(k.dtype), n, kr, vr, _int_vector(start, c.batch, "start"),
-                                              _int_vector(count, c.batch, "count"), _stream()))
+        k = torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=cache.pool.device)
+        v = torch.empty_like(k)
+    else:
+        k, v = out
+    dt = k.dtype
+    _check("vsa2_cache_read", _lib().vsa2_cache_read(
+        ctypes.byref(c), _vdtype(dt), n, ctypes.byref(_rows(k, shape, dt, "out")),
+        ctypes.byref(_rows(v, shape, dt, "out")), _vector(start, (batch,), torch.int32, "start"),
+        _vector(count, (batch,), torch.int32, "count"), _stream()))
     return k, v
 
 
@@ -792,20 +787,22 @@ def attn_cache(cache, q, length, count=None, causal=False, o=None):
     first length[b] list positions; causal: the call's tokens are the last
     count[b] (None: n) of them and see no later one.  Returns (o, lse), o like q
     and contiguous unless given, lse [batch, heads_q, n] fp32."""
-    torch = _torch()
-    c = cache.c
-    heads, n = q.shape[1], q.shape[2]
-    shape = (c.batch, heads, n, c.head_dim)
-    qr = _rows(q, shape, q.dtype, "q")
+    torch, c = _torch(), cache.c
+    i32, dt, batch = torch.int32, q.dtype, c.batch
+    shape = q.shape
+    heads, n = shape[1], shape[2]
+    want = (batch, heads, n, c.head_dim)
+    qr = _rows(q, want, dt, "q")
     if o is None:
-        o = torch.empty(shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(shape[:3], dtype=torch.float32, device=q.device)
-    st, wsb = vsa2_attn_cache_workspace(c, heads, n)
-    _check("vsa2_attn_cache_workspace", st)
+        o = q.new_empty(want)
+    lse = torch.empty(want[:3], dtype=torch.float32, device=q.device)
+    ref = ctypes.byref(c)
+    wsb = ctypes.c_size_t(0)
+    _check("vsa2_attn_cache_workspace", _lib().vsa2_attn_cache_workspace(ref, heads, n, ctypes.byref(wsb)))
+    wsb = wsb.value
     ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
-    _check("vsa2_attn_cache", vsa2_attn_cache(c, _vdtype(q.dtype), heads, n, qr,
-                                              _int_vector(length, c.batch, "length"),
-                                              _int_vector(count, c.batch, "count"), int(bool(causal)),
-                                              _rows(o, shape, q.dtype, "o"), lse.data_ptr(), _ptr(ws), wsb,
-                                              _stream()))
+    _check("vsa2_attn_cache", _lib().vsa2_attn_cache(
+        ref, _vdtype(dt), heads, n, ctypes.byref(qr), _vector(length, (batch,), i32, "length"),
+        _vector(count, (batch,), i32, "count"), 1 if causal else 0, ctypes.byref(_rows(o, want, dt, "o")),
+        lse.data_ptr(), _ptr(ws), wsb, _stream()))
     return o, lse

@@ -280,6 +280,34 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void norm_rope_kernel(rope_args a)
     }
 }
 
+// The norm's gradient in place: g with respect to the gained row -> to x; adds
+// the row's part of the gain's gradient to dg.
+template <int D>
+__device__ __forceinline__ void norm_back(float (&g0)[4], float (&g1)[4], float (&x0)[4], float (&x1)[4], float eps,
+                                          const float (&w)[2][4], float (&dg)[2][4]) {
+    float ss = 0.f, dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ss = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], ss));
+    const float r = rsqrtf(row_sum<D / 8>(ss) * (1.f / D) + eps);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x0[i] *= r;
+        x1[i] *= r;
+        const float e0 = g0[i] * x0[i], e1 = g1[i] * x1[i];
+        dg[0][i] += e0;
+        dg[1][i] += e1;
+        dot = fmaf(e0, w[0][i], fmaf(e1, w[1][i], dot));
+        g0[i] *= w[0][i];
+        g1[i] *= w[1][i];
+    }
+    const float mean = row_sum<D / 8>(dot) * (1.f / D);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        g0[i] = r * (g0[i] - x0[i] * mean);
+        g1[i] = r * (g1[i] - x1[i] * mean);
+    }
+}
+
 // Gradients.  The gains' gradients are sums over every token and head: each
 // lane adds up its 8 elements over the tokens and heads its wave walks over,
 // the workgroup joins its waves and rows in LDS and writes one partial row
@@ -320,9 +348,8 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void norm_rope_bwd_kernel(rope_arg
             for (int u = 0; u < AHEAD; ++u) {
                 int h;
                 const int hh = h0 + u * stride;
-                if (hh >= heads) break;
                 const int x = part_of(a, hh, h);
-                if (x < 2) {
+                if (hh < heads && x < 2) {
                     float g0[4], g1[4];
                     to_pairs<HALVES>(rg[u], g0, g1);
 #pragma unroll
@@ -332,39 +359,14 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void norm_rope_bwd_kernel(rope_arg
                         g0[i] = b0;
                     }
                     if (norm) {
-                        float x0[4], x1[4], ss = 0.f, dot = 0.f;
+                        float x0[4], x1[4];
                         to_pairs<HALVES>(rx[u], x0, x1);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) ss = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], ss));
-                        const float r = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + a.eps);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            x0[i] *= r;
-                            x1[i] *= r;
-                            const float e0 = g0[i] * x0[i], e1 = g1[i] * x1[i];
-                            if (x == 0) {
-                                dg[0][0][i] += e0;
-                                dg[0][1][i] += e1;
-                            } else {
-                                dg[1][0][i] += e0;
-                                dg[1][1][i] += e1;
-                            }
-                            const float w0 = x == 0 ? gain[0][0][i] : gain[1][0][i];
-                            const float w1 = x == 0 ? gain[0][1][i] : gain[1][1][i];
-                            dot = fmaf(e0, w0, fmaf(e1, w1, dot));
-                            g0[i] *= w0;
-                            g1[i] *= w1;
-                        }
-                        const float mean = row_sum<LPR>(dot) * (1.f / D);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            g0[i] = r * (g0[i] - x0[i] * mean);
-                            g1[i] = r * (g1[i] - x1[i] * mean);
-                        }
+                        if (x == 0) norm_back<D>(g0, g1, x0, x1, a.eps, gain[0], dg[0]);
+                        else norm_back<D>(g0, g1, x0, x1, a.eps, gain[1], dg[1]);
                     }
                     from_pairs<HALVES>(rg[u], g0, g1);
                 }
-                if (t.at >= 0) {
+                if (hh < heads && t.at >= 0) {
                     const row_view& out = a.part[x].dx;
                     store_raw<!HALVES>(rg[u], const_cast<T*>(row_at<T>(out, t, h)), a0, a1);
                 }
@@ -391,22 +393,26 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void norm_rope_bwd_kernel(rope_arg
     }
 }
 
-// Column sums of the partial rows [n][2 D]: a workgroup takes 64 columns, its
-// 16 waves every 16th row each.
+// Column sums of the partial rows [n][2 D]: a workgroup takes 16 columns, its
+// 64 groups of 16 lanes every 64th row each, four rows in flight.
 __global__ __launch_bounds__(1024) void norm_rope_gain_kernel(const float* partial, int64_t n, int D, float* dq_gain,
                                                               float* dk_gain) {
-    __shared__ float part[16][64];
-    const int lane = lane_id(), wave = wave_id(), col = blockIdx.x * 64 + lane;
-    float sum = 0.f;
-    for (int64_t r = wave; r < n; r += 16) sum += partial[r * 2 * D + col];
-    part[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0) {
-        sum = 0.f;
+    __shared__ float part[64][16];
+    const int lane = threadIdx.x & 15, slice = threadIdx.x >> 4, col = blockIdx.x * 16 + lane;
+    float sum[4] = {};
+    for (int64_t r = slice; r < n; r += 4 * 64) {
 #pragma unroll
-        for (int w = 0; w < 16; ++w) sum += part[w][lane];
+        for (int u = 0; u < 4; ++u)
+            if (r + 64 * u < n) sum[u] += partial[(r + 64 * u) * 2 * D + col];
+    }
+    part[slice][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 64; ++w) total += part[w][lane];
         float* out = col < D ? dq_gain : dk_gain;
-        if (out) out[col < D ? col : col - D] = sum;
+        if (out) out[col < D ? col : col - D] = total;
     }
 }
 
@@ -417,7 +423,7 @@ int head_split(int64_t groups, int heads) {
 }
 
 // Workgroups along the tokens in the gradients: each writes one partial row.
-constexpr int64_t BWD_GROUPS = 2048;
+constexpr int64_t BWD_GROUPS = 1024;
 
 }  // namespace
 
@@ -461,7 +467,7 @@ hipError_t launch_norm_rope_bwd(int dtype, int D, bool halves, const rope_args& 
     VSA2_ROPE_DISPATCH(norm_rope_bwd_kernel, grid);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.partial) return e;
-    hipLaunchKernelGGL(norm_rope_gain_kernel, dim3(2 * D / 64), dim3(1024), 0, s, a.partial, gx * gy, D, dq_gain,
+    hipLaunchKernelGGL(norm_rope_gain_kernel, dim3(2 * D / 16), dim3(1024), 0, s, a.partial, gx * gy, D, dq_gain,
                        dk_gain);
     return hipGetLastError();
 }

@@ -24,8 +24,9 @@ namespace {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896340f;
-constexpr int TILE = 16;          // rows of a workgroup
+constexpr int TILE = 16;          // rows of a workgroup of attn_cache_kernel
 constexpr int NW = 4;             // waves of a workgroup
+constexpr int ROWS = 32 * NW;     // rows of a workgroup of attn_cache_rows_kernel
 
 struct attn_args {
     cache_view c;
@@ -33,7 +34,7 @@ struct attn_args {
     float* lse;
     const int32_t* length;
     const int32_t* count;
-    float* part;         // [items][splits]: O [16][D], then (m, l) [16][2] of each
+    float* part;         // [items][splits]: O [tile rows][D], then (m, l) [tile rows][2] of each
     int n, group, rows, tiles, splits;
     bool causal;
 };
@@ -73,6 +74,12 @@ __device__ __forceinline__ f32x4_t mma16(const frag_bf16& a, const frag_bf16& b,
 }
 
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// 0xff in each byte that is a NaN code (0x7f or 0xff).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+    return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+}
+constexpr uint32_t ONE_E4M3 = 0x38383838u;     // four codes of 1.0
 
 __device__ __forceinline__ void store4(float* p, const float* x) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -199,15 +206,14 @@ __device__ __forceinline__ void page_step(const char* page, int64_t pos, int lim
             uint32_t w[4] = {vr[c].x & keep[0], vr[c].y & keep[1], vr[c].z & keep[2], vr[c].w & keep[3]}, nan[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                nan[t] = ((((w[t] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+                nan[t] = nan_bytes(w[t]);
                 w[t] &= ~nan[t];
             }
             vr[c] = make_uint4(w[0], w[1], w[2], w[3]);
             if (__ballot((nan[0] | nan[1] | nan[2] | nan[3]) != 0) != 0) {
                 f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                const uint32_t one = 0x38383838u;      // 1.0 in e4m3
-                hit = mma16(decode8(nan[0] & one, nan[1] & one, 1.f), pf[0][0], hit);
-                hit = mma16(decode8(nan[2] & one, nan[3] & one, 1.f), pf[1][0], hit);
+                hit = mma16(decode8(nan[0] & ONE_E4M3, nan[1] & ONE_E4M3, 1.f), pf[0][0], hit);
+                hit = mma16(decode8(nan[2] & ONE_E4M3, nan[3] & ONE_E4M3, 1.f), pf[1][0], hit);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
@@ -327,23 +333,337 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
     }
 }
 
-// Joins the splits of a row tile, in their order.
+// ---------------------------------------------------------------------------
+// Many rows: a wave takes 32 of them on 32x32x16 MFMAs, a workgroup's four waves
+// walk the same pages, copied into LDS asynchronously one page ahead.
+//
+// The page's order fits these fragments too: lane (half h, r = lane % 32) takes
+// K's 16-byte piece 2 w + h of token 32 T + r for two k-steps, and V's pieces
+// g = h and h + 2 of element 32 c + r, whose dwords t are the two runs of four
+// tokens that the accumulators of S^T hold for k-step t.  Reads are runs of
+// 256 bytes per 16 lanes: no bank conflicts, no padding, one address per lane.
+// ---------------------------------------------------------------------------
+typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+
+// Both halves' maximum of a column.
+__device__ __forceinline__ float halves_max(float x) { return fmaxf(x, swap_half(x)); }
+
+// Valid pages of a list's piece [lo, hi) in order: 64 table entries at a time in
+// a register, a bit for each that names a page.
+struct page_walk {
+    const int32_t* table;
+    int at, hi, pages;     // next entries to fetch; pages of the pool
+    int ids, base;         // fetched entries (one per lane), their first position
+    uint64_t left;         // of those, still to visit
+
+    __device__ __forceinline__ void fetch() {
+        const int x = at + lane_id();
+        ids = x < hi ? table[x] : -1;
+        left = __ballot(ids >= 0 && ids < pages);
+        base = at;
+        at += 64;
+    }
+    __device__ __forceinline__ page_walk(const int32_t* t, int lo, int hi_, int n) : table(t), at(lo), hi(hi_), pages(n) {
+        left = 0;
+        ids = -1;
+        base = lo;
+    }
+    // position and page of the next one; false at the end
+    __device__ __forceinline__ bool next(int& pos, int& id) {
+        while (left == 0) {
+            if (at >= hi) return false;
+            fetch();
+        }
+        const int bit = __builtin_ctzll(left);
+        left &= left - 1;
+        pos = base + bit;
+        id = __builtin_amdgcn_readlane(ids, bit);
+        return true;
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void copy_page(char* lds, const char* page, int wave, int lane) {
+    // 128 D bytes of codes: each wave 32 D of them in whole 1 KB copies
+    constexpr int NR = D / 32;
+    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void_t*)lds)) + wave * 32 * D;
+    const int from = wave * 32 * D + lane * 16 + DMA_BIAS;
+    const int off[4] = {from, from, from, from};      // the copies' own offsets step both sides
+    dma16_run<NR>(to, reinterpret_cast<uint64_t>(page) - DMA_BIAS, off);
+}
+
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a) {
-    const uint32_t item = blockIdx.x, bh = item / a.tiles;
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_rows_kernel(attn_args a) {
+    constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
+    __shared__ __attribute__((aligned(1024))) char codes[2][128 * D];
+    __shared__ __attribute__((aligned(16))) float power[NW][2][64];
+    const int lane = lane_id(), wave = wave_id(), h2 = lane >> 5, col = lane & 31;
+    uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
     const int tile = static_cast<int>(item % a.tiles);
+    item /= a.tiles;
+    const int split = static_cast<int>(item % a.splits);
+    const uint32_t bh = item / a.splits;
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
-    const int row = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), rr = tile * TILE + row;
+    const int r = tile * ROWS + wave * 32 + col;
+    const int limit = row_limit(a, b, r);
+    int wmin = limit, wmax = limit;
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+        wmin = min(wmin, __shfl_xor(wmin, m, 64));
+        wmax = max(wmax, __shfl_xor(wmax, m, 64));
+    }
+    wmin = __builtin_amdgcn_readfirstlane(wmin);
+    wmax = __builtin_amdgcn_readfirstlane(wmax);
+    __shared__ int most[NW];
+    if (lane == 0) most[wave] = wmax;
+    __syncthreads();
+    int all = most[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) all = max(all, most[w]);
+    all = __builtin_amdgcn_readfirstlane(all);
+    const int pages = (all + CACHE_TOKENS - 1) / CACHE_TOKENS;
+    const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
+    const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
+
+    frag_bf16 qf[KC][2][NT];
+    const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
+#pragma unroll
+    for (int w = 0; w < KC; ++w)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            float y[8] = {};
+            if (r < a.rows) {
+                const T* e = q + (2 * w + h2) * 16 + z * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
+            }
+            split_frag<NT>(qf[w][z], y);
+        }
+    f32x16_t o[VC];
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float scale = LOG2E / sqrtf(static_cast<float>(D));
+    const int kbase = (col >> 4) * (D / 64) * 1024 + h2 * 256 + (col & 15) * 16;
+    const int vbase = 64 * D + (col >> 4) * 1024 + h2 * 256 + (col & 15) * 16;
+    // in-page places of this lane's token's two powers
+    const int ke_at = 128 * D + (lane & 15) * 4 + (lane >> 4);
+    const int ve_at = 128 * D + 64 + ((lane >> 2) & 3) * 16 + (lane >> 4) * 4 + (lane & 3);
+
+    const int32_t* table =
+        a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
+    page_walk walk(table, lo, hi, a.c.pages);
+    int pos, id, npos = 0, nid = 0;
+    bool more = walk.next(pos, id);
+    auto page_at = [&](int x) {
+        return a.c.pool + (static_cast<int64_t>(x) * a.c.heads + h) * cache_page_bytes(D);
+    };
+    uint8_t ke = 0, ve = 0;
+    if (more) {
+        const char* page = page_at(id);
+        ke = static_cast<uint8_t>(page[ke_at]);
+        ve = static_cast<uint8_t>(page[ve_at]);
+        copy_page<D>(codes[0], page, wave, lane);
+    }
+    int buf = 0;
+    while (more) {
+        power[wave][0][lane] = power_of(ke);
+        power[wave][1][lane] = power_of(ve);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        wg_barrier();          // this page is in LDS, and the other buffer is done with
+        const bool next = walk.next(npos, nid);
+        if (next) {
+            const char* page = page_at(nid);
+            ke = static_cast<uint8_t>(page[ke_at]);
+            ve = static_cast<uint8_t>(page[ve_at]);
+            copy_page<D>(codes[buf ^ 1], page, wave, lane);
+        }
+        const int first = pos * CACHE_TOKENS;
+        if (first < wmax) {
+            const char* kp = codes[buf] + kbase;
+            const char* vp = codes[buf] + vbase;
+            f32x16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+                const float pw = power[wave][0][t * 32 + col];
+#pragma unroll
+                for (int w = 0; w < KC; ++w) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(kp + t * 2 * (D / 64) * 1024 + (w / 2) * 1024 + (w % 2) * 512);
+                    const frag_bf16 k0 = decode8(x.x, x.y, pw), k1 = decode8(x.z, x.w, pw);
+#pragma unroll
+                    for (int y = NT - 1; y >= 0; --y) {
+                        mma(s[t], k0, qf[w][0][y]);
+                        mma(s[t], k1, qf[w][1][y]);
+                    }
+                }
+            }
+            const bool masked = first + CACHE_TOKENS > wmin;
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= limit) s[t][i] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
+            mx = halves_max(mx) * scale;
+            // the running maximum moves only when it would grow by more than 8
+            // (weights up to 2^8 of the first): most pages leave O alone
+            if (__ballot(mx > m + 8.f) != 0) {
+                const float up = fmaxf(m, mx);
+                const float f = up == -INFINITY ? 1.f : fast_exp2(m - up);
+                m = up;
+                l *= f;
+#pragma unroll
+                for (int c = 0; c < VC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[c][i] *= f;
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+            frag_bf16 pf[4][NT];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    y[i] = fast_exp2(fmaf(s[t / 2][(t % 2) * 8 + i], scale, -base));
+                    l += y[i];
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float4 pw = *reinterpret_cast<const float4*>(&power[wave][1][t * 16 + x * 8 + 4 * h2]);
+                    const float pv[4] = {pw.x, pw.y, pw.z, pw.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // a masked place's power may be anything
+                        y[4 * x + i] = masked && y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
+                    }
+                }
+                split_frag<NT>(pf[t], y);
+            }
+            auto add_v = [&](int c, const uint4& x, const uint4& y) {
+                const uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const frag_bf16 vf = decode8(wx[t], wy[t], 1.f);
+#pragma unroll
+                    for (int z = NT - 1; z >= 0; --z) mma(o[c], vf, pf[t][z]);
+                }
+            };
+            if (!masked) {
+#pragma unroll
+                for (int c = 0; c < VC; ++c)
+                    add_v(c, *reinterpret_cast<const uint4*>(vp + c * 2048),
+                          *reinterpret_cast<const uint4*>(vp + c * 2048 + 512));
+            } else {
+                // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
+                uint32_t keep[4][2];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
+                        keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
+                    }
+#pragma unroll
+                for (int c = 0; c < VC; ++c) {
+                    const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
+                    const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
+                    uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
+                    uint32_t nan[4][2], any = 0;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            w[t][x] &= keep[t][x];
+                            nan[t][x] = nan_bytes(w[t][x]);
+                            w[t][x] &= ~nan[t][x];
+                            any |= nan[t][x];
+                        }
+                    if (__ballot(any != 0) != 0) {
+                        f32x16_t hit;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(hit[i] == 0.f)) o[c][i] = __uint_as_float(0x7fc00000u);
+                    }
+                    add_v(c, make_uint4(w[0][0], w[1][0], w[2][0], w[3][0]),
+                          make_uint4(w[0][1], w[1][1], w[2][1], w[3][1]));
+                }
+            }
+        }
+        more = next;
+        pos = npos;
+        id = nid;
+        buf ^= 1;
+    }
+    l += swap_half(l);
+    const float base = m == -INFINITY ? 0.f : m;
+    if (a.splits > 1) {
+        float* part = a.part + ((static_cast<int64_t>(bh) * a.tiles + tile) * a.splits + split) * (ROWS * (D + 2));
+        const int row = wave * 32 + col;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const float x[4] = {o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]};
+                store4(part + row * D + c * 32 + 2 * i + 4 * h2, x);
+            }
+        if (h2 == 0) {
+            part[ROWS * D + 2 * row] = m;
+            part[ROWS * D + 2 * row + 1] = l;
+        }
+        return;
+    }
+    if (r >= a.rows) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, r);
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            float x[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) x[y] = l == 0.f ? 0.f : o[c][i + y] * inv;
+            store4(out + c * 32 + 2 * i + 4 * h2, x);
+        }
+    if (h2 == 0) {
+        const int i = r / a.group, hg = r - i * a.group;
+        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
+    }
+}
+
+// Joins the splits of a row tile, in their order: a workgroup takes 16 rows.
+template <typename T, int D, int TR>
+__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a) {
+    constexpr int64_t STRIDE = TR * (D + 2);
+    const uint32_t item = blockIdx.x / (TR / 16), bh = item / a.tiles;
+    const int tile = static_cast<int>(item % a.tiles), sub = blockIdx.x % (TR / 16);
+    const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
+    const int row = sub * 16 + threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), rr = tile * TR + row;
     if (rr >= a.rows) return;
-    const float* part = a.part + static_cast<int64_t>(item) * a.splits * (TILE * (D + 2));
+    const float* part = a.part + static_cast<int64_t>(item) * a.splits * STRIDE;
     float m = -INFINITY;
-    for (int x = 0; x < a.splits; ++x) m = fmaxf(m, part[x * TILE * (D + 2) + TILE * D + 2 * row]);
+    for (int x = 0; x < a.splits; ++x) m = fmaxf(m, part[x * STRIDE + TR * D + 2 * row]);
     const float base = m == -INFINITY ? 0.f : m;
     float l = 0.f, o[D / 16] = {};
+#pragma unroll 4
     for (int x = 0; x < a.splits; ++x) {
-        const float* px = part + static_cast<int64_t>(x) * TILE * (D + 2);
-        const float f = fast_exp2(px[TILE * D + 2 * row] - base);
-        l += f * px[TILE * D + 2 * row + 1];
+        const float* px = part + x * STRIDE;
+        const float f = fast_exp2(px[TR * D + 2 * row] - base);
+        l += f * px[TR * D + 2 * row + 1];
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4) {
             const float4 y = *reinterpret_cast<const float4*>(px + row * D + d0 + i);
@@ -365,30 +685,38 @@ __global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a) {
     }
 }
 
-// Pieces a list is split into: enough workgroups for the chip, a page for every
-// wave at least.
-int split_count(const cache_view& c, int64_t tiles) {
-    const int64_t items = static_cast<int64_t>(c.batch) * c.heads * tiles;
-    const int64_t want = (1024 + items - 1) / items, most = (c.max_pages + NW - 1) / NW;
-    return static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
-}
+// How a call is cut: rows per workgroup, row tiles of a KV head, pieces of a list.
+struct attn_plan {
+    int tile_rows;
+    int64_t tiles;
+    int splits;
+};
 
-int64_t tiles_of(int heads_q, int heads, int n) {
-    return (static_cast<int64_t>(heads_q / heads) * n + TILE - 1) / TILE;
+attn_plan plan_attn(const cache_view& c, int heads_q, int n) {
+    attn_plan p;
+    const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n;
+    p.tile_rows = rows > 2 * TILE ? ROWS : TILE;
+    p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+    const int64_t items = static_cast<int64_t>(c.batch) * c.heads * p.tiles;
+    // enough workgroups for the chip, and a page for every wave at least
+    const int64_t fill = p.tile_rows == ROWS ? 512 : 1024, least = p.tile_rows == ROWS ? 8 : NW;
+    const int64_t want = fill / items, most = (c.max_pages + least - 1) / least;
+    p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+    return p;
 }
 
 }  // namespace
 
 size_t attn_cache_workspace_bytes(const cache_view& c, int D, int heads_q, int n) {
-    const int64_t tiles = tiles_of(heads_q, c.heads, n);
-    const int splits = split_count(c, tiles);
-    if (splits == 1) return 0;
-    return static_cast<size_t>(c.batch) * c.heads * tiles * splits * TILE * (D + 2) * sizeof(float);
+    const attn_plan p = plan_attn(c, heads_q, n);
+    if (p.splits == 1) return 0;
+    return static_cast<size_t>(c.batch) * c.heads * p.tiles * p.splits * p.tile_rows * (D + 2) * sizeof(float);
 }
 
 hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
                              const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
                              void* ws, hipStream_t s) {
+    const attn_plan p = plan_attn(c, heads_q, n);
     attn_args a{};
     a.c = c;
     a.q = q;
@@ -400,14 +728,22 @@ hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q,
     a.n = n;
     a.group = heads_q / c.heads;
     a.rows = a.group * n;
-    a.tiles = static_cast<int>(tiles_of(heads_q, c.heads, n));
-    a.splits = split_count(c, a.tiles);
+    a.tiles = static_cast<int>(p.tiles);
+    a.splits = p.splits;
     a.causal = causal;
-    const unsigned items = static_cast<unsigned>(static_cast<int64_t>(c.batch) * c.heads * a.tiles);
-#define VSA2_ATTN_GO(T, DD)                                                                                      \
-    do {                                                                                                         \
-        hipLaunchKernelGGL((attn_cache_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);          \
-        if (a.splits > 1) hipLaunchKernelGGL((attn_cache_join_kernel<T, DD>), dim3(items), dim3(256), 0, s, a);  \
+    const unsigned items = static_cast<unsigned>(static_cast<int64_t>(c.batch) * c.heads * p.tiles);
+#define VSA2_ATTN_GO(T, DD)                                                                                           \
+    do {                                                                                                              \
+        if (p.tile_rows == ROWS) {                                                                                    \
+            hipLaunchKernelGGL((attn_cache_rows_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);      \
+            if (a.splits > 1)                                                                                         \
+                hipLaunchKernelGGL((attn_cache_join_kernel<T, DD, ROWS>), dim3(items * (ROWS / 16)), dim3(256), 0, s, \
+                                   a);                                                                                \
+        } else {                                                                                                      \
+            hipLaunchKernelGGL((attn_cache_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);           \
+            if (a.splits > 1)                                                                                         \
+                hipLaunchKernelGGL((attn_cache_join_kernel<T, DD, TILE>), dim3(items), dim3(256), 0, s, a);           \
+        }                                                                                                             \
     } while (0)
     if (dtype == 0 && D == 64) VSA2_ATTN_GO(float, 64);
     else if (dtype == 0) VSA2_ATTN_GO(float, 128);

@@ -121,8 +121,10 @@ struct tile_state {
     f32x4_t o[D / 16];
 };
 
-template <typename T, int D>
-__device__ __forceinline__ void page_step(const char* page, int64_t pos, int limit, int lim_min, int lim_max,
+// One page for a tile.  MASKED: some row's limit, or the list's end, may lie
+// inside it.
+template <typename T, int D, bool MASKED>
+__device__ __forceinline__ void page_step(const char* page, int pos, int limit, int lim_max,
                                           const frag_bf16 (&qf)[D / 32][terms_of<T>], float scale,
                                           tile_state<D>& st) {
     constexpr int NT = terms_of<T>;
@@ -154,14 +156,13 @@ __device__ __forceinline__ void page_step(const char* page, int64_t pos, int lim
         }
     }
     const uint32_t vw[4] = {ve.x, ve.y, ve.z, ve.w};
-    const bool masked = pos + CACHE_TOKENS > lim_min;
     float p[4][4], mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float x = s[t][i] * scale;
-            if (masked && pos + 16 * t + 4 * g + i >= limit) x = -INFINITY;
+            if (MASKED && pos + 16 * t + 4 * g + i >= limit) x = -INFINITY;
             p[t][i] = x;
             mx = fmaxf(mx, x);
         }
@@ -178,7 +179,7 @@ __device__ __forceinline__ void page_step(const char* page, int64_t pos, int lim
             const float e = fast_exp2(p[t][i] - base);
             sum += e;
             // a masked place's power may be anything
-            p[t][i] = masked && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
+            p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
         }
     st.l = st.l * alpha + sum;
     frag_bf16 pf[2][NT];
@@ -190,7 +191,7 @@ __device__ __forceinline__ void page_step(const char* page, int64_t pos, int lim
     }
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) st.o[c] *= alpha;
-    if (masked) {
+    if constexpr (MASKED) {
         // Codes past every row's limit are whatever the page held: taken as
         // zeros.  A NaN below it, which some rows see and others do not, is
         // taken out of the product and given to the rows that see it (a second
@@ -198,8 +199,8 @@ __device__ __forceinline__ void page_step(const char* page, int64_t pos, int lim
         uint32_t keep[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int64_t left = lim_max - (pos + 16 * t + 4 * g);
-            keep[t] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * static_cast<int>(left)));
+            const int left = lim_max - (pos + 16 * t + 4 * g);
+            keep[t] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
         }
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
     const int r = tile * TILE + col;
     const int limit = row_limit(a, b, r);
     const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(limit));
-    const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(limit));
+    const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(r < a.rows ? limit : INT32_MAX));
     const int pages = (lim_max + CACHE_TOKENS - 1) / CACHE_TOKENS;
     const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
@@ -282,7 +283,8 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
         const int id = __builtin_amdgcn_readfirstlane(table[pg]);
         if (id < 0 || id >= a.c.pages) continue;
         const char* page = a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D);
-        page_step<T, D>(page, static_cast<int64_t>(pg) * CACHE_TOKENS, limit, lim_min, lim_max, qf, scale, st);
+        if ((pg + 1) * CACHE_TOKENS <= lim_min) page_step<T, D, false>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+        else page_step<T, D, true>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
     }
     st.l += __shfl_xor(st.l, 16, 64);
     st.l += __shfl_xor(st.l, 32, 64);
@@ -392,6 +394,135 @@ __device__ __forceinline__ void copy_page(char* lds, const char* page, int wave,
     dma16_run<NR>(to, reinterpret_cast<uint64_t>(page) - DMA_BIAS, off);
 }
 
+// A wave's 32 rows: running maximum and sum (base 2), O^T of column lane % 32,
+// elements 32 c + 8 (i / 4) + 4 (lane / 32) + i % 4.
+template <int D>
+struct rows_state {
+    float m, l;
+    f32x16_t o[D / 32];
+};
+
+// One page in LDS for a wave's rows.  MASKED: some row's limit, or the list's
+// end, may lie inside it.
+template <typename T, int D, bool MASKED>
+__device__ __forceinline__ void rows_step(const char* kp, const char* vp, const float (*power)[64], int first, int limit,
+                                          int wmax, const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale,
+                                          rows_state<D>& st) {
+    constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
+    const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
+    f32x16_t s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+        const float pw = power[0][t * 32 + col];
+#pragma unroll
+        for (int w = 0; w < KC; ++w) {
+            const uint4 x = *reinterpret_cast<const uint4*>(kp + t * 2 * (D / 64) * 1024 + (w / 2) * 1024 + (w % 2) * 512);
+            const frag_bf16 k0 = decode8(x.x, x.y, pw), k1 = decode8(x.z, x.w, pw);
+#pragma unroll
+            for (int y = NT - 1; y >= 0; --y) {
+                mma(s[t], k0, qf[w][0][y]);
+                mma(s[t], k1, qf[w][1][y]);
+            }
+        }
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= limit) s[t][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
+    mx = halves_max(mx) * scale;
+    // the running maximum moves only when it would grow by more than 8
+    // (weights up to 2^8 of the first): most pages leave O alone
+    if (__ballot(mx > st.m + 8.f) != 0) {
+        const float up = fmaxf(st.m, mx);
+        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
+        st.m = up;
+        st.l *= f;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
+    }
+    const float base = st.m == -INFINITY ? 0.f : st.m;
+    frag_bf16 pf[4][NT];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            y[i] = fast_exp2(fmaf(s[t / 2][(t % 2) * 8 + i], scale, -base));
+            st.l += y[i];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float4 pw = *reinterpret_cast<const float4*>(&power[1][t * 16 + x * 8 + 4 * h2]);
+            const float pv[4] = {pw.x, pw.y, pw.z, pw.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // a masked place's power may be anything
+                if constexpr (MASKED) y[4 * x + i] = y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
+                else y[4 * x + i] *= pv[i];
+            }
+        }
+        split_frag<NT>(pf[t], y);
+    }
+    uint32_t keep[4][2];
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
+                keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
+            }
+    }
+#pragma unroll
+    for (int c = 0; c < VC; ++c) {
+        const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
+        const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
+        uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
+        if constexpr (MASKED) {
+            // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
+            uint32_t nan[4][2], any = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    w[t][x] &= keep[t][x];
+                    nan[t][x] = nan_bytes(w[t][x]);
+                    w[t][x] &= ~nan[t][x];
+                    any |= nan[t][x];
+                }
+            if (__ballot(any != 0) != 0) {
+                f32x16_t hit;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const frag_bf16 vf = decode8(w[t][0], w[t][1], 1.f);
+#pragma unroll
+            for (int z = NT - 1; z >= 0; --z) mma(st.o[c], vf, pf[t][z]);
+        }
+    }
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_rows_kernel(attn_args a) {
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
@@ -406,21 +537,28 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
     const int r = tile * ROWS + wave * 32 + col;
     const int limit = row_limit(a, b, r);
-    int wmin = limit, wmax = limit;
+    // the rows' limits: the wave's largest, the workgroup's largest and (of rows that exist) smallest
+    int wmax = limit, wmin = r < a.rows ? limit : INT32_MAX;
 #pragma unroll
     for (int m = 16; m; m >>= 1) {
         wmin = min(wmin, __shfl_xor(wmin, m, 64));
         wmax = max(wmax, __shfl_xor(wmax, m, 64));
     }
-    wmin = __builtin_amdgcn_readfirstlane(wmin);
     wmax = __builtin_amdgcn_readfirstlane(wmax);
-    __shared__ int most[NW];
-    if (lane == 0) most[wave] = wmax;
+    __shared__ int ends[NW][2];
+    if (lane == 0) {
+        ends[wave][0] = wmin;
+        ends[wave][1] = wmax;
+    }
     __syncthreads();
-    int all = most[0];
+    int all = 0, full = INT32_MAX;
 #pragma unroll
-    for (int w = 1; w < NW; ++w) all = max(all, most[w]);
+    for (int w = 0; w < NW; ++w) {
+        full = min(full, ends[w][0]);
+        all = max(all, ends[w][1]);
+    }
     all = __builtin_amdgcn_readfirstlane(all);
+    full = __builtin_amdgcn_readfirstlane(full) / CACHE_TOKENS;     // pages before this one need no mask
     const int pages = (all + CACHE_TOKENS - 1) / CACHE_TOKENS;
     const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
@@ -439,12 +577,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
             }
             split_frag<NT>(qf[w][z], y);
         }
-    f32x16_t o[VC];
+    rows_state<D> st;
+    st.m = -INFINITY;
+    st.l = 0.f;
 #pragma unroll
     for (int c = 0; c < VC; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+        for (int i = 0; i < 16; ++i) st.o[c][i] = 0.f;
     const float scale = LOG2E / sqrtf(static_cast<float>(D));
     const int kbase = (col >> 4) * (D / 64) * 1024 + h2 * 256 + (col & 15) * 16;
     const int vbase = 64 * D + (col >> 4) * 1024 + h2 * 256 + (col & 15) * 16;
@@ -455,160 +594,45 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     const int32_t* table =
         a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
     page_walk walk(table, lo, hi, a.c.pages);
-    int pos, id, npos = 0, nid = 0;
-    bool more = walk.next(pos, id);
-    auto page_at = [&](int x) {
-        return a.c.pool + (static_cast<int64_t>(x) * a.c.heads + h) * cache_page_bytes(D);
-    };
+    int pos = 0, id = 0, buf = 0;
     uint8_t ke = 0, ve = 0;
-    if (more) {
-        const char* page = page_at(id);
+    bool more = walk.next(pos, id);
+    auto request = [&](int x, int to) {
+        const char* page = a.c.pool + (static_cast<int64_t>(x) * a.c.heads + h) * cache_page_bytes(D);
         ke = static_cast<uint8_t>(page[ke_at]);
         ve = static_cast<uint8_t>(page[ve_at]);
-        copy_page<D>(codes[0], page, wave, lane);
-    }
-    int buf = 0;
-    while (more) {
+        copy_page<D>(codes[to], page, wave, lane);
+    };
+    if (more) request(id, 0);
+    // Waits for the page at hand, requests the next one and says which was at
+    // hand.  Past the barrier every wave is done with the other buffer.
+    auto turn = [&](int& at) {
         power[wave][0][lane] = power_of(ke);
         power[wave][1][lane] = power_of(ve);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        wg_barrier();          // this page is in LDS, and the other buffer is done with
-        const bool next = walk.next(npos, nid);
-        if (next) {
-            const char* page = page_at(nid);
-            ke = static_cast<uint8_t>(page[ke_at]);
-            ve = static_cast<uint8_t>(page[ve_at]);
-            copy_page<D>(codes[buf ^ 1], page, wave, lane);
-        }
-        const int first = pos * CACHE_TOKENS;
-        if (first < wmax) {
-            const char* kp = codes[buf] + kbase;
-            const char* vp = codes[buf] + vbase;
-            f32x16_t s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-                const float pw = power[wave][0][t * 32 + col];
-#pragma unroll
-                for (int w = 0; w < KC; ++w) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(kp + t * 2 * (D / 64) * 1024 + (w / 2) * 1024 + (w % 2) * 512);
-                    const frag_bf16 k0 = decode8(x.x, x.y, pw), k1 = decode8(x.z, x.w, pw);
-#pragma unroll
-                    for (int y = NT - 1; y >= 0; --y) {
-                        mma(s[t], k0, qf[w][0][y]);
-                        mma(s[t], k1, qf[w][1][y]);
-                    }
-                }
-            }
-            const bool masked = first + CACHE_TOKENS > wmin;
-            if (masked) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= limit) s[t][i] = -INFINITY;
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
-            mx = halves_max(mx) * scale;
-            // the running maximum moves only when it would grow by more than 8
-            // (weights up to 2^8 of the first): most pages leave O alone
-            if (__ballot(mx > m + 8.f) != 0) {
-                const float up = fmaxf(m, mx);
-                const float f = up == -INFINITY ? 1.f : fast_exp2(m - up);
-                m = up;
-                l *= f;
-#pragma unroll
-                for (int c = 0; c < VC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[c][i] *= f;
-            }
-            const float base = m == -INFINITY ? 0.f : m;
-            frag_bf16 pf[4][NT];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    y[i] = fast_exp2(fmaf(s[t / 2][(t % 2) * 8 + i], scale, -base));
-                    l += y[i];
-                }
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float4 pw = *reinterpret_cast<const float4*>(&power[wave][1][t * 16 + x * 8 + 4 * h2]);
-                    const float pv[4] = {pw.x, pw.y, pw.z, pw.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // a masked place's power may be anything
-                        y[4 * x + i] = masked && y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
-                    }
-                }
-                split_frag<NT>(pf[t], y);
-            }
-            auto add_v = [&](int c, const uint4& x, const uint4& y) {
-                const uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const frag_bf16 vf = decode8(wx[t], wy[t], 1.f);
-#pragma unroll
-                    for (int z = NT - 1; z >= 0; --z) mma(o[c], vf, pf[t][z]);
-                }
-            };
-            if (!masked) {
-#pragma unroll
-                for (int c = 0; c < VC; ++c)
-                    add_v(c, *reinterpret_cast<const uint4*>(vp + c * 2048),
-                          *reinterpret_cast<const uint4*>(vp + c * 2048 + 512));
-            } else {
-                // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
-                uint32_t keep[4][2];
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
-                        keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
-                    }
-#pragma unroll
-                for (int c = 0; c < VC; ++c) {
-                    const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
-                    const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
-                    uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
-                    uint32_t nan[4][2], any = 0;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            w[t][x] &= keep[t][x];
-                            nan[t][x] = nan_bytes(w[t][x]);
-                            w[t][x] &= ~nan[t][x];
-                            any |= nan[t][x];
-                        }
-                    if (__ballot(any != 0) != 0) {
-                        f32x16_t hit;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) hit[i] = 0.f;
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!(hit[i] == 0.f)) o[c][i] = __uint_as_float(0x7fc00000u);
-                    }
-                    add_v(c, make_uint4(w[0][0], w[1][0], w[2][0], w[3][0]),
-                          make_uint4(w[0][1], w[1][1], w[2][1], w[3][1]));
-                }
-            }
-        }
-        more = next;
-        pos = npos;
-        id = nid;
+        wg_barrier();
+        at = pos;
+        more = walk.next(pos, id);
+        if (more) request(id, buf ^ 1);
+    };
+    while (more && pos < full) {
+        int at;
+        turn(at);
+        rows_step<T, D, false>(codes[buf] + kbase, codes[buf] + vbase, power[wave], at * CACHE_TOKENS, limit, wmax, qf,
+                               scale, st);
         buf ^= 1;
     }
+    while (more) {
+        int at;
+        turn(at);
+        if (at * CACHE_TOKENS < wmax)
+            rows_step<T, D, true>(codes[buf] + kbase, codes[buf] + vbase, power[wave], at * CACHE_TOKENS, limit, wmax, qf,
+                                  scale, st);
+        buf ^= 1;
+    }
+    const float m = st.m;
+    float l = st.l;
+    f32x16_t(&o)[VC] = st.o;
     l += swap_half(l);
     const float base = m == -INFINITY ? 0.f : m;
     if (a.splits > 1) {

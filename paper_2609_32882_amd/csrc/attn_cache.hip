@@ -27,6 +27,7 @@ constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896340f;
 constexpr int TILE = 16;          // rows of a workgroup of attn_cache_kernel
 constexpr int NW = 4;             // waves of a workgroup
 constexpr int ROWS = 32 * NW;     // rows of a workgroup of attn_cache_rows_kernel
+constexpr int STAGE = 2;          // pages it copies at a time
 
 struct attn_args {
     cache_view c;
@@ -348,7 +349,11 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
 
 // Both halves' maximum of a column.
-__device__ __forceinline__ float halves_max(float x) { return fmaxf(x, swap_half(x)); }
+__device__ __forceinline__ float halves_max(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
 
 // Valid pages of a list's piece [lo, hi) in order: 64 table entries at a time in
 // a register, a bit for each that names a page.
@@ -402,9 +407,9 @@ struct rows_state {
     f32x16_t o[D / 32];
 };
 
-// One page in LDS for a wave's rows.  MASKED: some row's limit, or the list's
-// end, may lie inside it.
-template <typename T, int D, bool MASKED>
+// One page in LDS for a wave's rows, where some row's limit, or the list's end,
+// may lie inside it.
+template <typename T, int D>
 __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const float (*power)[64], int first, int limit,
                                           int wmax, const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale,
                                           rows_state<D>& st) {
@@ -427,13 +432,11 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
             }
         }
     }
-    if constexpr (MASKED) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= limit) s[t][i] = -INFINITY;
-    }
+        for (int i = 0; i < 16; ++i)
+            if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= limit) s[t][i] = -INFINITY;
     float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -469,50 +472,45 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 // a masked place's power may be anything
-                if constexpr (MASKED) y[4 * x + i] = y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
-                else y[4 * x + i] *= pv[i];
+                y[4 * x + i] = y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
             }
         }
         split_frag<NT>(pf[t], y);
     }
     uint32_t keep[4][2];
-    if constexpr (MASKED) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
-                keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
-            }
-    }
+        for (int x = 0; x < 2; ++x) {
+            const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
+            keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
+        }
 #pragma unroll
     for (int c = 0; c < VC; ++c) {
         const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
         const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
         uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
-        if constexpr (MASKED) {
-            // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
-            uint32_t nan[4][2], any = 0;
+        // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
+        uint32_t nan[4][2], any = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                w[t][x] &= keep[t][x];
+                nan[t][x] = nan_bytes(w[t][x]);
+                w[t][x] &= ~nan[t][x];
+                any |= nan[t][x];
+            }
+        if (__ballot(any != 0) != 0) {
+            f32x16_t hit;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) hit[i] = 0.f;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
+                mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    w[t][x] &= keep[t][x];
-                    nan[t][x] = nan_bytes(w[t][x]);
-                    w[t][x] &= ~nan[t][x];
-                    any |= nan[t][x];
-                }
-            if (__ballot(any != 0) != 0) {
-                f32x16_t hit;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) hit[i] = 0.f;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
-            }
+            for (int i = 0; i < 16; ++i)
+                if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -523,11 +521,90 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
     }
 }
 
+// The two pages of a stage together, no limit inside either.
+template <typename T, int D>
+__device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase, const float (*power)[2][64],
+                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale, rows_state<D>& st) {
+    constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
+    const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
+    f32x16_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const char* kp = lds + (t / 2) * 128 * D + kbase;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+        const float pw = power[t / 2][0][(t % 2) * 32 + col];
+#pragma unroll
+        for (int w = 0; w < KC; ++w) {
+            const uint4 x = *reinterpret_cast<const uint4*>(kp + (t % 2) * 2 * (D / 64) * 1024 + (w / 2) * 1024 + (w % 2) * 512);
+            const frag_bf16 k0 = decode8(x.x, x.y, pw), k1 = decode8(x.z, x.w, pw);
+#pragma unroll
+            for (int y = NT - 1; y >= 0; --y) {
+                mma(s[t], k0, qf[w][0][y]);
+                mma(s[t], k1, qf[w][1][y]);
+            }
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
+    mx = halves_max(mx) * scale;
+    if (__ballot(mx > st.m + 8.f) != 0) {
+        const float up = fmaxf(st.m, mx);
+        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
+        st.m = up;
+        st.l *= f;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
+    }
+    const float base = st.m == -INFINITY ? 0.f : st.m;
+    float l2[2] = {0.f, 0.f};
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg) {
+        const char* vp = lds + pg * 128 * D + vbase;
+        frag_bf16 pf[4][NT];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                y[i] = fast_exp2(fmaf(s[2 * pg + t / 2][(t % 2) * 8 + i], scale, -base));
+                l2[i & 1] += y[i];
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float4 pw = *reinterpret_cast<const float4*>(&power[pg][1][t * 16 + x * 8 + 4 * h2]);
+                const float pv[4] = {pw.x, pw.y, pw.z, pw.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[4 * x + i] *= pv[i];
+            }
+            split_frag<NT>(pf[t], y);
+        }
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+            const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
+            const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
+            const uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const frag_bf16 vf = decode8(w[t][0], w[t][1], 1.f);
+#pragma unroll
+                for (int z = NT - 1; z >= 0; --z) mma(st.o[c], vf, pf[t][z]);
+            }
+        }
+    }
+    st.l += l2[0] + l2[1];
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_rows_kernel(attn_args a) {
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
-    __shared__ __attribute__((aligned(1024))) char codes[2][128 * D];
-    __shared__ __attribute__((aligned(16))) float power[NW][2][64];
+    __shared__ __attribute__((aligned(1024))) char codes[2][STAGE][128 * D];
+    __shared__ __attribute__((aligned(16))) float power[NW][STAGE][2][64];
     const int lane = lane_id(), wave = wave_id(), h2 = lane >> 5, col = lane & 31;
     uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
     const int tile = static_cast<int>(item % a.tiles);
@@ -594,40 +671,53 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     const int32_t* table =
         a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
     page_walk walk(table, lo, hi, a.c.pages);
-    int pos = 0, id = 0, buf = 0;
-    uint8_t ke = 0, ve = 0;
-    bool more = walk.next(pos, id);
-    auto request = [&](int x, int to) {
-        const char* page = a.c.pool + (static_cast<int64_t>(x) * a.c.heads + h) * cache_page_bytes(D);
-        ke = static_cast<uint8_t>(page[ke_at]);
-        ve = static_cast<uint8_t>(page[ve_at]);
-        copy_page<D>(codes[to], page, wave, lane);
+    int pos[STAGE], buf = 0, have = 0;
+    uint8_t ke[STAGE] = {}, ve[STAGE] = {};
+    auto request = [&](int to) {
+        have = 0;
+#pragma unroll
+        for (int x = 0; x < STAGE; ++x) {
+            int id;
+            pos[x] = 0;
+            if (have < x || !walk.next(pos[x], id)) continue;
+            const char* page = a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D);
+            ke[x] = static_cast<uint8_t>(page[ke_at]);
+            ve[x] = static_cast<uint8_t>(page[ve_at]);
+            copy_page<D>(codes[to][x], page, wave, lane);
+            have = x + 1;
+        }
     };
-    if (more) request(id, 0);
-    // Waits for the page at hand, requests the next one and says which was at
+    request(0);
+    // Waits for the pages at hand, requests the next ones and says which were at
     // hand.  Past the barrier every wave is done with the other buffer.
-    auto turn = [&](int& at) {
-        power[wave][0][lane] = power_of(ke);
-        power[wave][1][lane] = power_of(ve);
+    int at[STAGE];
+    auto turn = [&]() {
+#pragma unroll
+        for (int x = 0; x < STAGE; ++x) {
+            power[wave][x][0][lane] = power_of(ke[x]);
+            power[wave][x][1][lane] = power_of(ve[x]);
+            at[x] = pos[x];
+        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         wg_barrier();
-        at = pos;
-        more = walk.next(pos, id);
-        if (more) request(id, buf ^ 1);
+        const int n = have;
+        request(buf ^ 1);
+        return n;
     };
-    while (more && pos < full) {
-        int at;
-        turn(at);
-        rows_step<T, D, false>(codes[buf] + kbase, codes[buf] + vbase, power[wave], at * CACHE_TOKENS, limit, wmax, qf,
-                               scale, st);
+    while (have == STAGE && pos[STAGE - 1] < full) {
+        turn();
+        rows_pair<T, D>(codes[buf][0], kbase, vbase, power[wave], qf, scale, st);
         buf ^= 1;
     }
-    while (more) {
-        int at;
-        turn(at);
-        if (at * CACHE_TOKENS < wmax)
-            rows_step<T, D, true>(codes[buf] + kbase, codes[buf] + vbase, power[wave], at * CACHE_TOKENS, limit, wmax, qf,
-                                  scale, st);
+    while (have > 0) {
+        const int n = turn();
+#pragma unroll 1
+        for (int x = 0; x < n; ++x) {
+            const int first = (x ? at[STAGE - 1] : at[0]) * CACHE_TOKENS;
+            if (first < wmax)
+                rows_step<T, D>(codes[buf][x] + kbase, codes[buf][x] + vbase, power[wave][x], first, limit, wmax, qf,
+                                      scale, st);
+        }
         buf ^= 1;
     }
     const float m = st.m;
@@ -722,10 +812,27 @@ attn_plan plan_attn(const cache_view& c, int heads_q, int n) {
     p.tile_rows = rows > 2 * TILE ? ROWS : TILE;
     p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t items = static_cast<int64_t>(c.batch) * c.heads * p.tiles;
-    // enough workgroups for the chip, and a page for every wave at least
-    const int64_t fill = p.tile_rows == ROWS ? 512 : 1024, least = p.tile_rows == ROWS ? 8 : NW;
-    const int64_t want = fill / items, most = (c.max_pages + least - 1) / least;
-    p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+    if (p.tile_rows == TILE) {
+        // enough workgroups for the chip, and a page for every wave at least
+        const int64_t want = 1024 / items, most = (c.max_pages + NW - 1) / NW;
+        p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+        return p;
+    }
+    // Rounds of the 512 resident workgroups, against the one that evenly spread
+    // work would take; a split adds the partial results' way to memory and back,
+    // which measured 1% of a list of 36,000 tokens.
+    const int64_t most = (c.max_pages + 7) / 8;
+    double best = 0.;
+    p.splits = 1;
+    for (int64_t n_splits = 1; n_splits <= most && (n_splits == 1 || items * n_splits <= 8 * 512); ++n_splits) {
+        const int64_t rounds = (items * n_splits + 511) / 512;
+        const double cost = static_cast<double>(rounds) / n_splits +
+                            (n_splits > 1 ? n_splits * 360. / (64. * c.max_pages) * items / 512. : 0.);
+        if (n_splits == 1 || cost < best) {
+            best = cost;
+            p.splits = static_cast<int>(n_splits);
+        }
+    }
     return p;
 }
 

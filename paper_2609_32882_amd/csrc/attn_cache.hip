@@ -25,8 +25,8 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896340f;
 constexpr int TILE = 16;          // rows of a workgroup of attn_cache_kernel
-constexpr int NW = 4;             // waves of a workgroup
-constexpr int ROWS = 32 * NW;     // rows of a workgroup of attn_cache_rows_kernel
+constexpr int NW = 4;             // waves of a workgroup of attn_cache_rows_kernel
+constexpr int ROWS = 32 * NW;     // its rows
 constexpr int STAGE = 2;          // pages it copies at a time
 
 struct attn_args {
@@ -114,6 +114,54 @@ __device__ __forceinline__ int row_limit(const attn_args& a, int b, int r) {
     return static_cast<int>(len < 0 ? 0 : len);
 }
 
+// Both halves' (all four 16-lane groups') maximum of a column.
+__device__ __forceinline__ float halves_max(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ __forceinline__ float groups_max(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return halves_max(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
+}
+
+// Valid pages of a list's piece [lo, hi) in order: 64 table entries at a time in
+// a register, a bit for each that names a page.
+struct page_walk {
+    const int32_t* table;
+    int at, hi, pages;     // next entries to fetch; pages of the pool
+    int ids, base;         // fetched entries (one per lane), their first position
+    uint64_t left;         // of those, still to visit
+
+    __device__ __forceinline__ page_walk(const int32_t* t, int lo, int hi_, int n)
+        : table(t), at(lo), hi(hi_), pages(n), ids(-1), base(lo), left(0) {}
+    // `mine`: which of 64 entries in a row the caller visits
+    __device__ __forceinline__ void fetch(uint64_t mine) {
+        const int x = at + lane_id();
+        ids = x < hi ? table[x] : -1;
+        left = __ballot(ids >= 0 && ids < pages) & mine;
+        base = at;
+        at += 64;
+    }
+    // position and page of the next one; false at the end
+    __device__ __forceinline__ bool next(int& pos, int& id, uint64_t mine = ~0ull) {
+        while (left == 0) {
+            if (at >= hi) return false;
+            fetch(mine);
+        }
+        const int bit = __builtin_ctzll(left);
+        left &= left - 1;
+        pos = base + bit;
+        id = __builtin_amdgcn_readlane(ids, bit);
+        return true;
+    }
+};
+
+__device__ __forceinline__ const int32_t* list_of(const attn_args& a, int b, int h) {
+    return a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
+}
+
 // One row tile's state in one wave: its running maximum and sum (base 2) and
 // O^T, rows d = 16 c + 4 g + i, column lane % 16.
 template <int D>
@@ -143,33 +191,32 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
     f32x4_t s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         const float power = power_of((ke >> (8 * t)) & 0xffu);
+        s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < D / 64; ++u) {
             const uint4 w = kr[t * (D / 64) + u];
             const frag_bf16 k0 = decode8(w.x, w.y, power), k1 = decode8(w.z, w.w, power);
 #pragma unroll
-            for (int x = NT - 1; x >= 0; --x) {
-                s[t] = mma16(k0, qf[2 * u][x], s[t]);
-                s[t] = mma16(k1, qf[2 * u + 1][x], s[t]);
+            for (int y = NT - 1; y >= 0; --y) {
+                s[t] = mma16(k0, qf[2 * u][y], s[t]);
+                s[t] = mma16(k1, qf[2 * u + 1][y], s[t]);
             }
         }
     }
     const uint32_t vw[4] = {ve.x, ve.y, ve.z, ve.w};
+    frag_bf16 pf[2][NT];
     float p[4][4], mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float x = s[t][i] * scale;
-            if (MASKED && pos + 16 * t + 4 * g + i >= limit) x = -INFINITY;
-            p[t][i] = x;
-            mx = fmaxf(mx, x);
+            float y = s[t][i] * scale;
+            if (MASKED && pos + 16 * t + 4 * g + i >= limit) y = -INFINITY;
+            p[t][i] = y;
+            mx = fmaxf(mx, y);
         }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float m = fmaxf(st.m, mx), base = m == -INFINITY ? 0.f : m;
+    const float m = fmaxf(st.m, groups_max(mx)), base = m == -INFINITY ? 0.f : m;
     const float alpha = fast_exp2(st.m - base);
     st.m = m;
     float sum = 0.f;
@@ -183,12 +230,11 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
             p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
         }
     st.l = st.l * alpha + sum;
-    frag_bf16 pf[2][NT];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const float y[8] = {p[2 * x][0], p[2 * x][1], p[2 * x][2], p[2 * x][3],
-                            p[2 * x + 1][0], p[2 * x + 1][1], p[2 * x + 1][2], p[2 * x + 1][3]};
-        split_frag<NT>(pf[x], y);
+    for (int y = 0; y < 2; ++y) {
+        const float z[8] = {p[2 * y][0], p[2 * y][1], p[2 * y][2], p[2 * y][3],
+                            p[2 * y + 1][0], p[2 * y + 1][1], p[2 * y + 1][2], p[2 * y + 1][3]};
+        split_frag<NT>(pf[y], z);
     }
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) st.o[c] *= alpha;
@@ -226,9 +272,9 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
     for (int c = 0; c < D / 16; ++c) {
         const frag_bf16 v0 = decode8(vr[c].x, vr[c].y, 1.f), v1 = decode8(vr[c].z, vr[c].w, 1.f);
 #pragma unroll
-        for (int x = NT - 1; x >= 0; --x) {
-            st.o[c] = mma16(v0, pf[0][x], st.o[c]);
-            st.o[c] = mma16(v1, pf[1][x], st.o[c]);
+        for (int y = NT - 1; y >= 0; --y) {
+            st.o[c] = mma16(v0, pf[0][y], st.o[c]);
+            st.o[c] = mma16(v1, pf[1][y], st.o[c]);
         }
     }
 }
@@ -238,12 +284,17 @@ __device__ __forceinline__ int64_t row_offset(const row_view& v, const attn_args
     const int i = r / a.group, hg = r - i * a.group;
     return b * v.batch + static_cast<int64_t>(h * a.group + hg) * v.head + static_cast<int64_t>(i) * v.token;
 }
+__device__ __forceinline__ void store_lse(const attn_args& a, int b, int h, int r, float base, float l) {
+    const int i = r / a.group, hg = r - i * a.group;
+    a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
+}
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
-    constexpr int NT = terms_of<T>;
-    __shared__ float so[NW][TILE][D + 4];
-    __shared__ float sml[NW][TILE][2];
+// Few rows: WAVES waves take turns at the list's pages, each for all the rows.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attn_cache_kernel(attn_args a) {
+    constexpr int NT = terms_of<T>, TR = TILE;
+    __shared__ float so[WAVES][TR][D + 4];
+    __shared__ float sml[WAVES][TR][2];
     const int lane = lane_id(), wave = wave_id(), g = lane >> 4, col = lane & 15;
     // row tiles of a list's piece share its pages: next to each other on one XCD
     uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
@@ -252,25 +303,31 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
     const int split = static_cast<int>(item % a.splits);
     const uint32_t bh = item / a.splits;
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
-    const int r = tile * TILE + col;
+    const int r = tile * TR + col;
     const int limit = row_limit(a, b, r);
     const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(limit));
     const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(r < a.rows ? limit : INT32_MAX));
     const int pages = (lim_max + CACHE_TOKENS - 1) / CACHE_TOKENS;
     const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
+    uint64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < 64; i += WAVES) mine |= 1ull << i;
+    mine <<= wave;
+    page_walk walk(list_of(a, b, h), lo, hi, a.c.pages);
+    if (lo < hi) walk.fetch(mine);
 
     frag_bf16 qf[D / 32][NT];
     const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x) {
+    for (int u = 0; u < D / 32; ++u) {
         float y[8] = {};
         if (r < a.rows) {
-            const T* e = q + (x / 2) * 64 + g * 16 + (x & 1) * 8;
+            const T* e = q + (u / 2) * 64 + g * 16 + (u & 1) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
         }
-        split_frag<NT>(qf[x], y);
+        split_frag<NT>(qf[u], y);
     }
     tile_state<D> st;
     st.m = -INFINITY;
@@ -278,61 +335,56 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) st.o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const float scale = LOG2E / sqrtf(static_cast<float>(D));
-    const int32_t* table =
-        a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
-    for (int pg = lo + wave; pg < hi; pg += NW) {
-        const int id = __builtin_amdgcn_readfirstlane(table[pg]);
-        if (id < 0 || id >= a.c.pages) continue;
+    int pg, id;
+    while (walk.next(pg, id, mine)) {
         const char* page = a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D);
-        if ((pg + 1) * CACHE_TOKENS <= lim_min) page_step<T, D, false>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
-        else page_step<T, D, true>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+        if ((pg + 1) * CACHE_TOKENS <= lim_min)
+            page_step<T, D, false>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+        else
+            page_step<T, D, true>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
     }
     st.l += __shfl_xor(st.l, 16, 64);
     st.l += __shfl_xor(st.l, 32, 64);
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) so[wave][col][16 * c + 4 * g + i] = st.o[c][i];
+    for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4_t*>(&so[wave][col][16 * c + 4 * g]) = st.o[c];
     if (g == 0) {
         sml[wave][col][0] = st.m;
         sml[wave][col][1] = st.l;
     }
     __syncthreads();
-    // join the waves: thread (row, D/16 elements)
-    const int row = threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16);
-    float m = sml[0][row][0];
+    // join the waves: a thread takes 4 elements of a row
+    for (int at = threadIdx.x; at < TR * (D / 4); at += 64 * WAVES) {
+        const int row = at / (D / 4), d0 = at % (D / 4) * 4, rr = tile * TR + row;
+        if (rr >= a.rows && a.splits == 1) continue;
+        float m = sml[0][row][0];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) m = fmaxf(m, sml[w][row][0]);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[D / 16] = {};
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sml[w][row][0]);
+        const float base = m == -INFINITY ? 0.f : m;
+        float l = 0.f, o[4] = {};
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        const float f = fast_exp2(sml[w][row][0] - base);
-        l += f * sml[w][row][1];
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] += f * so[w][row][d0 + i];
-    }
-    const int rr = tile * TILE + row;
-    if (a.splits > 1) {
-        float* part = a.part + ((static_cast<int64_t>(bh) * a.tiles + tile) * a.splits + split) * (TILE * (D + 2));
-#pragma unroll
-        for (int i = 0; i < D / 16; i += 4) store4(part + row * D + d0 + i, o + i);
-        if (threadIdx.x % 16 == 0) {
-            part[TILE * D + 2 * row] = m;
-            part[TILE * D + 2 * row + 1] = l;
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = fast_exp2(sml[w][row][0] - base);
+            const float4 y = *reinterpret_cast<const float4*>(&so[w][row][d0]);
+            l += f * sml[w][row][1];
+            o[0] += f * y.x;
+            o[1] += f * y.y;
+            o[2] += f * y.z;
+            o[3] += f * y.w;
         }
-        return;
-    }
-    if (rr >= a.rows) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (a.splits > 1) {
+            float* part = a.part + ((static_cast<int64_t>(bh) * a.tiles + tile) * a.splits + split) * (TR * (D + 2));
+            store4(part + row * D + d0, o);
+            if (d0 == 0) {
+                part[TR * D + 2 * row] = m;
+                part[TR * D + 2 * row + 1] = l;
+            }
+            continue;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
-    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + d0;
-#pragma unroll
-    for (int i = 0; i < D / 16; i += 4) store4(out + i, o + i);
-    if (threadIdx.x % 16 == 0) {
-        const int i = rr / a.group, hg = rr - i * a.group;
-        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
+        for (int i = 0; i < 4; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
+        store4(static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + d0, o);
+        if (d0 == 0) store_lse(a, b, h, rr, base, l);
     }
 }
 
@@ -347,47 +399,6 @@ __global__ __launch_bounds__(64 * NW) void attn_cache_kernel(attn_args a) {
 // 256 bytes per 16 lanes: no bank conflicts, no padding, one address per lane.
 // ---------------------------------------------------------------------------
 typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
-
-// Both halves' maximum of a column.
-__device__ __forceinline__ float halves_max(float x) {
-    const uint32_t u = __float_as_uint(x);
-    const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-}
-
-// Valid pages of a list's piece [lo, hi) in order: 64 table entries at a time in
-// a register, a bit for each that names a page.
-struct page_walk {
-    const int32_t* table;
-    int at, hi, pages;     // next entries to fetch; pages of the pool
-    int ids, base;         // fetched entries (one per lane), their first position
-    uint64_t left;         // of those, still to visit
-
-    __device__ __forceinline__ void fetch() {
-        const int x = at + lane_id();
-        ids = x < hi ? table[x] : -1;
-        left = __ballot(ids >= 0 && ids < pages);
-        base = at;
-        at += 64;
-    }
-    __device__ __forceinline__ page_walk(const int32_t* t, int lo, int hi_, int n) : table(t), at(lo), hi(hi_), pages(n) {
-        left = 0;
-        ids = -1;
-        base = lo;
-    }
-    // position and page of the next one; false at the end
-    __device__ __forceinline__ bool next(int& pos, int& id) {
-        while (left == 0) {
-            if (at >= hi) return false;
-            fetch();
-        }
-        const int bit = __builtin_ctzll(left);
-        left &= left - 1;
-        pos = base + bit;
-        id = __builtin_amdgcn_readlane(ids, bit);
-        return true;
-    }
-};
 
 template <int D>
 __device__ __forceinline__ void copy_page(char* lds, const char* page, int wave, int lane) {
@@ -668,9 +679,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     const int ke_at = 128 * D + (lane & 15) * 4 + (lane >> 4);
     const int ve_at = 128 * D + 64 + ((lane >> 2) & 3) * 16 + (lane >> 4) * 4 + (lane & 3);
 
-    const int32_t* table =
-        a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
-    page_walk walk(table, lo, hi, a.c.pages);
+    page_walk walk(list_of(a, b, h), lo, hi, a.c.pages);
     int pos[STAGE], buf = 0, have = 0;
     uint8_t ke[STAGE] = {}, ve[STAGE] = {};
     auto request = [&](int to) {
@@ -753,84 +762,106 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
             for (int y = 0; y < 4; ++y) x[y] = l == 0.f ? 0.f : o[c][i + y] * inv;
             store4(out + c * 32 + 2 * i + 4 * h2, x);
         }
-    if (h2 == 0) {
-        const int i = r / a.group, hg = r - i * a.group;
-        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
-    }
+    if (h2 == 0) store_lse(a, b, h, r, base, l);
 }
 
-// Joins the splits of a row tile, in their order: a workgroup takes 16 rows.
-template <typename T, int D, int TR>
-__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a) {
-    constexpr int64_t STRIDE = TR * (D + 2);
-    const uint32_t item = blockIdx.x / (TR / 16), bh = item / a.tiles;
-    const int tile = static_cast<int>(item % a.tiles), sub = blockIdx.x % (TR / 16);
+// Joins the pieces of a row tile, in their order: a workgroup takes 8 rows, 32
+// lanes each.  The lanes first work out the pieces' weights, 32 at a time.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a, int tile_rows) {
+    const int64_t stride = static_cast<int64_t>(tile_rows) * (D + 2);
+    const int subs = tile_rows / 8;
+    const uint32_t item = blockIdx.x / subs, bh = item / a.tiles;
+    const int tile = static_cast<int>(item % a.tiles), sub = static_cast<int>(blockIdx.x % subs);
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
-    const int row = sub * 16 + threadIdx.x / 16, d0 = (threadIdx.x % 16) * (D / 16), rr = tile * TR + row;
-    if (rr >= a.rows) return;
-    const float* part = a.part + static_cast<int64_t>(item) * a.splits * STRIDE;
+    const int lane = threadIdx.x & 31, row = sub * 8 + (threadIdx.x >> 5), rr = tile * tile_rows + row;
+    if (rr >= a.rows) return;             // the 32 lanes of a row together
+    const float* part = a.part + static_cast<int64_t>(item) * a.splits * stride;
+    const float* ml = part + static_cast<int64_t>(tile_rows) * D + 2 * row;
     float m = -INFINITY;
-    for (int x = 0; x < a.splits; ++x) m = fmaxf(m, part[x * STRIDE + TR * D + 2 * row]);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[D / 16] = {};
-#pragma unroll 4
-    for (int x = 0; x < a.splits; ++x) {
-        const float* px = part + x * STRIDE;
-        const float f = fast_exp2(px[TR * D + 2 * row] - base);
-        l += f * px[TR * D + 2 * row + 1];
+    for (int x = lane; x < a.splits; x += 32) m = fmaxf(m, ml[x * stride]);
 #pragma unroll
-        for (int i = 0; i < D / 16; i += 4) {
-            const float4 y = *reinterpret_cast<const float4*>(px + row * D + d0 + i);
-            o[i] += f * y.x;
-            o[i + 1] += f * y.y;
-            o[i + 2] += f * y.z;
-            o[i + 3] += f * y.w;
+    for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k, 64));
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[D / 32] = {};
+    for (int x0 = 0; x0 < a.splits; x0 += 32) {
+        float f = 0.f;
+        if (x0 + lane < a.splits) {
+            const float2 y = *reinterpret_cast<const float2*>(ml + (x0 + lane) * stride);
+            f = fast_exp2(y.x - base);
+            l += f * y.y;
+        }
+        const int n = min(32, a.splits - x0);
+        const float* px = part + x0 * stride + row * D + lane * (D / 32);
+#pragma unroll 4
+        for (int x = 0; x < n; ++x) {
+            const float w = __shfl(f, (threadIdx.x & 32) + x, 64);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) o[i] += w * px[x * stride + i];
         }
     }
+#pragma unroll
+    for (int k = 16; k; k >>= 1) l += __shfl_xor(l, k, 64);
     const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + lane * (D / 32);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i] = l == 0.f ? 0.f : o[i] * inv;
-    T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + d0;
-#pragma unroll
-    for (int i = 0; i < D / 16; i += 4) store4(out + i, o + i);
-    if (threadIdx.x % 16 == 0) {
-        const int i = rr / a.group, hg = rr - i * a.group;
-        a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
-    }
+    for (int i = 0; i < D / 32; ++i) from_f32(out[i], l == 0.f ? 0.f : o[i] * inv);
+    if (lane == 0) store_lse(a, b, h, rr, base, l);
 }
 
-// How a call is cut: rows per workgroup, row tiles of a KV head, pieces of a list.
+// How a call is cut: rows per workgroup and its waves, row tiles of a KV head,
+// pieces of a list.
 struct attn_plan {
-    int tile_rows;
+    int tile_rows, waves;
     int64_t tiles;
     int splits;
 };
 
-attn_plan plan_attn(const cache_view& c, int heads_q, int n) {
+// Which kernel: 16-row tiles whose waves share out a list's pages, or 128-row
+// tiles whose waves share the pages.  The first reads a page once per 16 rows
+// but splits finely; measured over lists of 20,000 tokens, D = 128 (us, 16-row
+// against 128-row tiles): bf16, 8 lists of 128 rows 34 against 44, 16 of 80
+// rows 45 against 52, 32 of 80 rows 77 against 73, of 128 rows 99 against 76,
+// 128 lists of 32, 64 and 128 rows 137 / 203 / 342 against 154 / 202 / 224;
+// fp32, 128 lists of 64, 96 and 128 rows 287 / 407 / 511 against 432 / 471 / 508.
+bool takes_tiles(int dtype, int64_t lists, int64_t rows) {
+    return rows <= 64 || (rows <= 128 && (dtype == 0 || lists < 32));
+}
+
+attn_plan plan_attn(int dtype, const cache_view& c, int heads_q, int n) {
     attn_plan p;
-    const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n;
-    p.tile_rows = rows > 2 * TILE ? ROWS : TILE;
-    p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
-    const int64_t items = static_cast<int64_t>(c.batch) * c.heads * p.tiles;
-    if (p.tile_rows == TILE) {
-        // enough workgroups for the chip, and a page for every wave at least
-        const int64_t want = 1024 / items, most = (c.max_pages + NW - 1) / NW;
+    const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n, heads = static_cast<int64_t>(c.batch) * c.heads;
+    if (takes_tiles(dtype, heads, rows)) {
+        p.tile_rows = TILE;
+        p.tiles = (rows + TILE - 1) / TILE;
+        // A short list stays in one piece, whose eight waves join it without a
+        // second launch; else enough workgroups of four waves for the chip, and a
+        // page for every wave at least.
+        if (p.tiles == 1 && c.max_pages <= 32) {
+            p.waves = 8;
+            p.splits = 1;
+            return p;
+        }
+        p.waves = 4;
+        const int64_t want = 1024 / (heads * p.tiles), most = (c.max_pages + 3) / 4;
         p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
         return p;
     }
+    p.tile_rows = ROWS;
+    p.waves = NW;
+    p.tiles = (rows + ROWS - 1) / ROWS;
     // Rounds of the 512 resident workgroups, against the one that evenly spread
     // work would take; a split adds the partial results' way to memory and back,
     // which measured 1% of a list of 36,000 tokens.
-    const int64_t most = (c.max_pages + 7) / 8;
+    const int64_t items = heads * p.tiles, most = (c.max_pages + 7) / 8;
     double best = 0.;
     p.splits = 1;
-    for (int64_t n_splits = 1; n_splits <= most && (n_splits == 1 || items * n_splits <= 8 * 512); ++n_splits) {
-        const int64_t rounds = (items * n_splits + 511) / 512;
-        const double cost = static_cast<double>(rounds) / n_splits +
-                            (n_splits > 1 ? n_splits * 360. / (64. * c.max_pages) * items / 512. : 0.);
-        if (n_splits == 1 || cost < best) {
+    for (int64_t k = 1; k <= most && (k == 1 || items * k <= 8 * 512); ++k) {
+        const int64_t rounds = (items * k + 511) / 512;
+        const double cost = static_cast<double>(rounds) / k + (k > 1 ? k * 360. / (64. * c.max_pages) * items / 512. : 0.);
+        if (k == 1 || cost < best) {
             best = cost;
-            p.splits = static_cast<int>(n_splits);
+            p.splits = static_cast<int>(k);
         }
     }
     return p;
@@ -839,15 +870,36 @@ attn_plan plan_attn(const cache_view& c, int heads_q, int n) {
 }  // namespace
 
 size_t attn_cache_workspace_bytes(const cache_view& c, int D, int heads_q, int n) {
-    const attn_plan p = plan_attn(c, heads_q, n);
-    if (p.splits == 1) return 0;
-    return static_cast<size_t>(c.batch) * c.heads * p.tiles * p.splits * p.tile_rows * (D + 2) * sizeof(float);
+    size_t most = 0;
+    for (int dtype = 0; dtype < 2; ++dtype) {
+        const attn_plan p = plan_attn(dtype, c, heads_q, n);
+        const size_t need = p.splits == 1 ? 0 : static_cast<size_t>(c.batch) * c.heads * p.tiles * p.splits *
+                                                    p.tile_rows * (D + 2) * sizeof(float);
+        if (need > most) most = need;
+    }
+    return most;
 }
+
+namespace {
+
+template <typename T, int D>
+void launch_attn(const attn_args& a, const attn_plan& p, hipStream_t s) {
+    const int64_t items = static_cast<int64_t>(a.c.batch) * a.c.heads * p.tiles;
+    const dim3 grid(static_cast<unsigned>(items * p.splits)), block(64 * p.waves);
+    if (p.tile_rows == ROWS) hipLaunchKernelGGL((attn_cache_rows_kernel<T, D>), grid, block, 0, s, a);
+    else if (p.waves == 8) hipLaunchKernelGGL((attn_cache_kernel<T, D, 8>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((attn_cache_kernel<T, D, 4>), grid, block, 0, s, a);
+    if (p.splits > 1)
+        hipLaunchKernelGGL((attn_cache_join_kernel<T, D>), dim3(static_cast<unsigned>(items * (p.tile_rows / 8))),
+                           dim3(256), 0, s, a, p.tile_rows);
+}
+
+}  // namespace
 
 hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
                              const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
                              void* ws, hipStream_t s) {
-    const attn_plan p = plan_attn(c, heads_q, n);
+    const attn_plan p = plan_attn(dtype, c, heads_q, n);
     attn_args a{};
     a.c = c;
     a.q = q;
@@ -862,25 +914,10 @@ hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q,
     a.tiles = static_cast<int>(p.tiles);
     a.splits = p.splits;
     a.causal = causal;
-    const unsigned items = static_cast<unsigned>(static_cast<int64_t>(c.batch) * c.heads * p.tiles);
-#define VSA2_ATTN_GO(T, DD)                                                                                           \
-    do {                                                                                                              \
-        if (p.tile_rows == ROWS) {                                                                                    \
-            hipLaunchKernelGGL((attn_cache_rows_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);      \
-            if (a.splits > 1)                                                                                         \
-                hipLaunchKernelGGL((attn_cache_join_kernel<T, DD, ROWS>), dim3(items * (ROWS / 16)), dim3(256), 0, s, \
-                                   a);                                                                                \
-        } else {                                                                                                      \
-            hipLaunchKernelGGL((attn_cache_kernel<T, DD>), dim3(items * a.splits), dim3(64 * NW), 0, s, a);           \
-            if (a.splits > 1)                                                                                         \
-                hipLaunchKernelGGL((attn_cache_join_kernel<T, DD, TILE>), dim3(items), dim3(256), 0, s, a);           \
-        }                                                                                                             \
-    } while (0)
-    if (dtype == 0 && D == 64) VSA2_ATTN_GO(float, 64);
-    else if (dtype == 0) VSA2_ATTN_GO(float, 128);
-    else if (D == 64) VSA2_ATTN_GO(bf16_t, 64);
-    else VSA2_ATTN_GO(bf16_t, 128);
-#undef VSA2_ATTN_GO
+    if (dtype == 0 && D == 64) launch_attn<float, 64>(a, p, s);
+    else if (dtype == 0) launch_attn<float, 128>(a, p, s);
+    else if (D == 64) launch_attn<bf16_t, 64>(a, p, s);
+    else launch_attn<bf16_t, 128>(a, p, s);
     return hipGetLastError();
 }
 

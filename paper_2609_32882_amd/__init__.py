@@ -709,8 +709,7 @@ def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, 
     dgain, ws, wsb = [None, None], None, 0
     if eps > 0 and (dq is not None or dk is not None):
         dev = (dq if dq is not None else dk).device
-        both = torch.empty((2, D), dtype=torch.float32, device=dev)
-        dgain = [both[0] if dq is not None else None, both[1] if dk is not None else None]
+        dgain = [None if g is None else torch.empty(D, dtype=torch.float32, device=dev) for g in (dq, dk)]
         st, wsb = vsa2_qk_norm_rope_workspace(p)
         _check("vsa2_qk_norm_rope_workspace", st)
         ws = torch.empty(wsb, dtype=torch.uint8, device=dev)

@@ -765,17 +765,22 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     if (h2 == 0) store_lse(a, b, h, r, base, l);
 }
 
-// Joins the pieces of a row tile, in their order: a workgroup takes 8 rows, 32
-// lanes each.  The lanes first work out the pieces' weights, 32 at a time.
-template <typename T, int D>
+// Joins the pieces of a row tile.  A row is joined by SLICES groups of 32 lanes,
+// each taking every SLICES-th piece, whose sums are added in order: one group
+// (8 rows a workgroup) for up to 8 pieces, eight groups for more, where one
+// group's loads one after the other took longer than the pieces themselves.
+template <typename T, int D, int SLICES>
 __global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a, int tile_rows) {
+    constexpr int RPW = 8 / SLICES;       // rows of a workgroup
+    __shared__ float so[SLICES > 1 ? SLICES : 1][D], sl[SLICES];
     const int64_t stride = static_cast<int64_t>(tile_rows) * (D + 2);
-    const int subs = tile_rows / 8;
+    const int subs = tile_rows / RPW;
     const uint32_t item = blockIdx.x / subs, bh = item / a.tiles;
     const int tile = static_cast<int>(item % a.tiles), sub = static_cast<int>(blockIdx.x % subs);
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
-    const int lane = threadIdx.x & 31, row = sub * 8 + (threadIdx.x >> 5), rr = tile * tile_rows + row;
-    if (rr >= a.rows) return;             // the 32 lanes of a row together
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, slice = group % SLICES;
+    const int row = sub * RPW + group / SLICES, rr = tile * tile_rows + row;
+    if (rr >= a.rows) return;             // all lanes of a row together (SLICES > 1: the workgroup)
     const float* part = a.part + static_cast<int64_t>(item) * a.splits * stride;
     const float* ml = part + static_cast<int64_t>(tile_rows) * D + 2 * row;
     float m = -INFINITY;
@@ -784,24 +789,38 @@ __global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a, int t
     for (int k = 16; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k, 64));
     const float base = m == -INFINITY ? 0.f : m;
     float l = 0.f, o[D / 32] = {};
-    for (int x0 = 0; x0 < a.splits; x0 += 32) {
+    // 32 of this slice's pieces at a time: their weights one a lane, then their sums
+    for (int x0 = slice; x0 < a.splits; x0 += 32 * SLICES) {
         float f = 0.f;
-        if (x0 + lane < a.splits) {
-            const float2 y = *reinterpret_cast<const float2*>(ml + (x0 + lane) * stride);
+        if (x0 + lane * SLICES < a.splits) {
+            const float2 y = *reinterpret_cast<const float2*>(ml + (x0 + lane * SLICES) * stride);
             f = fast_exp2(y.x - base);
             l += f * y.y;
         }
-        const int n = min(32, a.splits - x0);
+        const int n = min(32, (a.splits - x0 + SLICES - 1) / SLICES);
         const float* px = part + x0 * stride + row * D + lane * (D / 32);
 #pragma unroll 4
         for (int x = 0; x < n; ++x) {
             const float w = __shfl(f, (threadIdx.x & 32) + x, 64);
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) o[i] += w * px[x * stride + i];
+            for (int i = 0; i < D / 32; ++i) o[i] += w * px[x * SLICES * stride + i];
         }
     }
 #pragma unroll
     for (int k = 16; k; k >>= 1) l += __shfl_xor(l, k, 64);
+    if constexpr (SLICES > 1) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) so[slice][lane * (D / 32) + i] = o[i];
+        if (lane == 0) sl[slice] = l;
+        __syncthreads();
+        if (slice) return;
+#pragma unroll
+        for (int x = 1; x < SLICES; ++x) {
+            l += sl[x];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) o[i] += so[x][lane * (D / 32) + i];
+        }
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, rr) + lane * (D / 32);
 #pragma unroll
@@ -835,15 +854,17 @@ attn_plan plan_attn(int dtype, const cache_view& c, int heads_q, int n) {
         p.tile_rows = TILE;
         p.tiles = (rows + TILE - 1) / TILE;
         // A short list stays in one piece, whose eight waves join it without a
-        // second launch; else enough workgroups of four waves for the chip, and a
-        // page for every wave at least.
+        // second launch; else the 512 workgroups of four waves that are resident
+        // at once (D = 128), and a page for every wave at least.  One token over
+        // 200,000: 1,024 workgroups 118 us, 512 85 (join included), 256 82; 20
+        // rows of 8 lists of 30,000 tokens 107 / 101 / 107.
         if (p.tiles == 1 && c.max_pages <= 32) {
             p.waves = 8;
             p.splits = 1;
             return p;
         }
         p.waves = 4;
-        const int64_t want = 1024 / (heads * p.tiles), most = (c.max_pages + 3) / 4;
+        const int64_t want = 512 / (heads * p.tiles), most = (c.max_pages + 3) / 4;
         p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
         return p;
     }
@@ -889,9 +910,11 @@ void launch_attn(const attn_args& a, const attn_plan& p, hipStream_t s) {
     if (p.tile_rows == ROWS) hipLaunchKernelGGL((attn_cache_rows_kernel<T, D>), grid, block, 0, s, a);
     else if (p.waves == 8) hipLaunchKernelGGL((attn_cache_kernel<T, D, 8>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((attn_cache_kernel<T, D, 4>), grid, block, 0, s, a);
-    if (p.splits > 1)
-        hipLaunchKernelGGL((attn_cache_join_kernel<T, D>), dim3(static_cast<unsigned>(items * (p.tile_rows / 8))),
-                           dim3(256), 0, s, a, p.tile_rows);
+    const auto rows_of = [&](int per_wg) { return dim3(static_cast<unsigned>(items * (p.tile_rows / per_wg))); };
+    if (p.splits > 8)
+        hipLaunchKernelGGL((attn_cache_join_kernel<T, D, 8>), rows_of(1), dim3(256), 0, s, a, p.tile_rows);
+    else if (p.splits > 1)
+        hipLaunchKernelGGL((attn_cache_join_kernel<T, D, 1>), rows_of(8), dim3(256), 0, s, a, p.tile_rows);
 }
 
 }  // namespace

@@ -591,22 +591,23 @@ def unpool_add(p, dx_c, dx, P):
 # norm + rotation + layout, the 8-bit cache and attention over it
 # --------------------------------------------------------------------------
 
-def _rows(t, shape, dtype, name):
-    """vsa2_rows of t [batch, heads, tokens, D] with any strides but D's."""
-    stride = t.stride()
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or stride[3] != 1:
-        raise ValueError("%s: expected %s %s on the GPU with contiguous rows, got %s %s strides %s" %
-                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape), tuple(stride)))
-    return vsa2_rows(t.data_ptr(), stride[0], stride[1], stride[2])
+_MARSHAL = None
 
 
-def _vector(t, shape, dtype, name):
-    """Pointer of a contiguous GPU tensor of that shape and dtype, or None."""
-    if t is None:
-        return None
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        _expect(t, shape, dtype, name)
-    return t.data_ptr()
+def _marshal():
+    """The host module _host.so: it takes these helpers' tensors, checks them,
+    makes their outputs and calls the C-ABI, at a third of ctypes' host time."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        _lib(), _torch()            # the libraries it links against
+        try:
+            from . import _host
+        except ImportError as e:
+            raise ImportError("_host.so is not built for this torch; run paper_2609_32882_amd/build.py "
+                              "(or __graft_entry__.build()): %s" % e) from e
+        _host.set_error(Vsa2Error)
+        _MARSHAL = _host
+    return _MARSHAL
 
 
 def _vdtype(dtype):
@@ -637,27 +638,18 @@ class Rope:
     PAIRINGS = {"adjacent": VSA2_ROPE_ADJACENT, "halves": VSA2_ROPE_HALVES}
 
     def __init__(self, axes, tables, origin=None, pairing="adjacent"):
-        torch = _torch()
+        self.c = vsa2_rope()
         pairs = self.PAIRINGS[pairing]
-        rows, ptrs = [0, 0, 0], [None, None, None]
-        for i, n in enumerate(axes):
-            if n:
-                t = tables[i]
-                if t is None:
-                    raise ValueError("tables[%d]: an axis of %d elements needs one" % (i, n))
-                rows[i] = t.shape[0]
-                ptrs[i] = _vector(t, (rows[i], n // 2, 2), torch.float32, "tables")
-        at = None if origin is None else _vector(origin, (origin.shape[0], 3), torch.int32, "origin")
-        self.c = vsa2_rope(tuple(axes), tuple(rows), tuple(ptrs), at, pairs)
+        _marshal().fill_rope(self.c, axes, tables, origin, pairs)
         self.tables, self.origin = tables, origin       # kept alive with their addresses
 
 
-def _rope_ref(rope, p):
+def _rope_c(rope, p):
     if rope is None:
         return None
     if rope.origin is not None and rope.origin.shape[0] != p.batch:
         raise ValueError("origin: expected %d sequences, got %d" % (p.batch, rope.origin.shape[0]))
-    return ctypes.byref(rope.c)
+    return rope.c
 
 
 def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None, eps=0.0, out=None):
@@ -666,22 +658,8 @@ def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None,
     [batch, heads_kv, tokens, D] in raster order, the grid and then the text
     (views of a fused projection are fine); each may be None.  Returns (q, k, v)
     contiguous; `out` gives the three outputs."""
-    torch = _torch()
     p = problem_from(p)
-    dt, batch, D, L = _tdtype(p), p.batch, p.head_dim, _joint(p)[1]
-    n = p.T * p.H * p.W + p.text_len
-    rows, ptrs, outs = [None] * 3, [None] * 3, [None] * 3
-    for i, x in enumerate((q, k, v)):
-        if x is None:
-            continue
-        heads = p.heads_kv if i else p.heads_q
-        rows[i] = ctypes.byref(_rows(x, (batch, heads, n, D), dt, "qkv"[i]))
-        y = outs[i] = x.new_empty((batch, heads, L, D)) if out is None else out[i]
-        ptrs[i] = _vector(y, (batch, heads, L, D), dt, "out")
-    _check("vsa2_qk_norm_rope", _lib().vsa2_qk_norm_rope(
-        ctypes.byref(p), _rope_ref(rope, p), eps, rows[0], _vector(q_gain, (D,), torch.float32, "q_gain"), ptrs[0],
-        rows[1], _vector(k_gain, (D,), torch.float32, "k_gain"), ptrs[1], rows[2], ptrs[2], _stream()))
-    return tuple(outs)
+    return _marshal().norm_rope(p, _rope_c(rope, p), eps, q, k, v, q_gain, k_gain, out, _stream)
 
 
 def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, k_gain=None, rope=None, eps=0.0,
@@ -691,33 +669,8 @@ def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, 
     forward's inputs ([batch, heads, tokens, D]; `out` gives them, views of one
     fused gradient are fine).  q and k are the forward's inputs, needed with the
     norm; the gains' gradients come with them."""
-    torch = _torch()
     p = problem_from(p)
-    dt, batch, D, L = _tdtype(p), p.batch, p.head_dim, _joint(p)[1]
-    n = p.T * p.H * p.W + p.text_len
-    dy, x_rows, dx_rows, dx = [None] * 3, [None] * 3, [None] * 3, [None] * 3
-    for i, (g, x) in enumerate(((dq, q), (dk, k), (dv, None))):
-        if g is None:
-            continue
-        heads = p.heads_kv if i else p.heads_q
-        shape = (batch, heads, n, D)
-        dy[i] = _vector(g, (batch, heads, L, D), dt, ("dq", "dk", "dv")[i])
-        dx[i] = g.new_empty((batch, n, heads, D)).transpose(1, 2) if out is None else out[i]
-        dx_rows[i] = ctypes.byref(_rows(dx[i], shape, dt, "out"))
-        if x is not None:
-            x_rows[i] = ctypes.byref(_rows(x, shape, dt, "qk"[i]))
-    dgain, ws, wsb = [None, None], None, 0
-    if eps > 0 and (dq is not None or dk is not None):
-        dev = (dq if dq is not None else dk).device
-        dgain = [None if g is None else torch.empty(D, dtype=torch.float32, device=dev) for g in (dq, dk)]
-        st, wsb = vsa2_qk_norm_rope_workspace(p)
-        _check("vsa2_qk_norm_rope_workspace", st)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=dev)
-    _check("vsa2_qk_norm_rope_bwd", _lib().vsa2_qk_norm_rope_bwd(
-        ctypes.byref(p), _rope_ref(rope, p), eps, x_rows[0], _vector(q_gain, (D,), torch.float32, "q_gain"), dy[0],
-        dx_rows[0], _ptr(dgain[0]), x_rows[1], _vector(k_gain, (D,), torch.float32, "k_gain"), dy[1], dx_rows[1],
-        _ptr(dgain[1]), dy[2], dx_rows[2], _ptr(ws), wsb, _stream()))
-    return dx[0], dx[1], dx[2], dgain[0], dgain[1]
+    return _marshal().norm_rope_bwd(p, _rope_c(rope, p), eps, dq, dk, dv, q, k, q_gain, k_gain, out, _stream)
 
 
 class KVCache:
@@ -728,17 +681,9 @@ class KVCache:
     __slots__ = ("c", "pool", "table")
 
     def __init__(self, pool, table):
-        torch = _torch()
-        shape, lists = pool.shape, table.shape
-        if len(shape) != 3 or shape[2] < 256 or (shape[2] - 128) % 128:
-            raise ValueError("pool: expected [pages, heads_kv, 128*D + 128], got %s" % (tuple(shape),))
-        if len(lists) != 2 and (len(lists) != 3 or lists[1] != shape[1]):
-            raise ValueError("table: expected [batch, max_pages] or [batch, %d, max_pages], got %s" %
-                             (shape[1], tuple(lists)))
-        self.c = vsa2_cache(lists[0], shape[1], (shape[2] - 128) // 128, shape[0], lists[-1],
-                            1 if len(lists) == 2 else lists[1], _vector(pool, shape, torch.uint8, "pool"),
-                            _vector(table, lists, torch.int32, "table"))
-        self.pool, self.table = pool, table
+        self.c = vsa2_cache()
+        _marshal().fill_cache(self.c, pool, table)
+        self.pool, self.table = pool, table             # kept alive with their addresses
 
     @classmethod
     def empty(cls, table, pages, heads_kv, head_dim):
@@ -752,33 +697,16 @@ def cache_write(cache, k, v, start, count=None):
     """Quantise tokens k, v [batch, heads_kv, n, D] (any strides) into the cache:
     token i < count[b] (int32 [batch], None: all n) goes to list position
     start[b] + i (int32 [batch])."""
-    i32, c = _torch().int32, cache.c
-    batch, dt = c.batch, k.dtype
-    shape = (batch, c.heads_kv, k.shape[2], c.head_dim)
-    _check("vsa2_cache_write", _lib().vsa2_cache_write(
-        ctypes.byref(c), _vdtype(dt), shape[2], ctypes.byref(_rows(k, shape, dt, "k")),
-        ctypes.byref(_rows(v, shape, dt, "v")), _vector(start, (batch,), i32, "start"),
-        _vector(count, (batch,), i32, "count"), _stream()))
+    _marshal().cache_write(cache.c, k, v, start, count, _stream)
 
 
 def cache_read(cache, n, start, count=None, dtype=None, out=None):
     """(k, v) [batch, heads_kv, n, D] of list positions start[b] .. start[b] + n - 1
     (zeros past count[b] and where the list has no page); bf16 unless `dtype`
     says float32.  `out` gives the two outputs (any strides)."""
-    torch, c = _torch(), cache.c
-    batch = c.batch
-    shape = (batch, c.heads_kv, n, c.head_dim)
-    if out is None:
-        k = torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=cache.pool.device)
-        v = torch.empty_like(k)
-    else:
-        k, v = out
-    dt = k.dtype
-    _check("vsa2_cache_read", _lib().vsa2_cache_read(
-        ctypes.byref(c), _vdtype(dt), n, ctypes.byref(_rows(k, shape, dt, "out")),
-        ctypes.byref(_rows(v, shape, dt, "out")), _vector(start, (batch,), torch.int32, "start"),
-        _vector(count, (batch,), torch.int32, "count"), _stream()))
-    return k, v
+    dt = VSA2_BF16 if dtype is None else _vdtype(dtype)
+    k, v = (None, None) if out is None else out
+    return _marshal().cache_read(cache.c, cache.pool, n, start, count, dt, k, v, _stream)
 
 
 def attn_cache(cache, q, length, count=None, causal=False, o=None):
@@ -786,22 +714,4 @@ def attn_cache(cache, q, length, count=None, causal=False, o=None):
     first length[b] list positions; causal: the call's tokens are the last
     count[b] (None: n) of them and see no later one.  Returns (o, lse), o like q
     and contiguous unless given, lse [batch, heads_q, n] fp32."""
-    torch, c = _torch(), cache.c
-    i32, dt, batch = torch.int32, q.dtype, c.batch
-    shape = q.shape
-    heads, n = shape[1], shape[2]
-    want = (batch, heads, n, c.head_dim)
-    qr = _rows(q, want, dt, "q")
-    if o is None:
-        o = q.new_empty(want)
-    lse = torch.empty(want[:3], dtype=torch.float32, device=q.device)
-    ref = ctypes.byref(c)
-    wsb = ctypes.c_size_t(0)
-    _check("vsa2_attn_cache_workspace", _lib().vsa2_attn_cache_workspace(ref, heads, n, ctypes.byref(wsb)))
-    wsb = wsb.value
-    ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
-    _check("vsa2_attn_cache", _lib().vsa2_attn_cache(
-        ref, _vdtype(dt), heads, n, ctypes.byref(qr), _vector(length, (batch,), i32, "length"),
-        _vector(count, (batch,), i32, "count"), 1 if causal else 0, ctypes.byref(_rows(o, want, dt, "o")),
-        lse.data_ptr(), _ptr(ws), wsb, _stream()))
-    return o, lse
+    return _marshal().attn_cache(cache.c, q, length, count, True if causal else False, o, _stream)

@@ -139,7 +139,11 @@ struct page_walk {
     // `mine`: which of 64 entries in a row the caller visits
     __device__ __forceinline__ void fetch(uint64_t mine) {
         const int x = at + lane_id();
-        ids = x < hi ? table[x] : -1;
+        start(x < hi ? table[x] : -1, mine);
+    }
+    // the same with the entries at hand (lane i: entry at + i, whatever it is past hi)
+    __device__ __forceinline__ void start(int entry, uint64_t mine) {
+        ids = at + lane_id() < hi ? entry : -1;
         left = __ballot(ids >= 0 && ids < pages) & mine;
         base = at;
         at += 64;
@@ -205,39 +209,47 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
         }
     }
     const uint32_t vw[4] = {ve.x, ve.y, ve.z, ve.w};
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (pos + 16 * t + 4 * g + i >= limit) s[t][i] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
+    mx = groups_max(mx) * scale;
+    // the running maximum moves only when it would grow by more than 8
+    // (weights up to 2^8 of the first): most pages leave O alone
+    if (__ballot(mx > st.m + 8.f) != 0) {
+        const float up = fmaxf(st.m, mx);
+        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
+        st.m = up;
+        st.l *= f;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) st.o[c] *= f;
+    }
+    const float base = st.m == -INFINITY ? 0.f : st.m;
     frag_bf16 pf[2][NT];
-    float p[4][4], mx = -INFINITY;
+    float p[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float y = s[t][i] * scale;
-            if (MASKED && pos + 16 * t + 4 * g + i >= limit) y = -INFINITY;
-            p[t][i] = y;
-            mx = fmaxf(mx, y);
-        }
-    const float m = fmaxf(st.m, groups_max(mx)), base = m == -INFINITY ? 0.f : m;
-    const float alpha = fast_exp2(st.m - base);
-    st.m = m;
-    float sum = 0.f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float e = fast_exp2(p[t][i] - base);
-            sum += e;
+            const float e = fast_exp2(fmaf(s[t][i], scale, -base));
+            st.l += e;
             // a masked place's power may be anything
             p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
         }
-    st.l = st.l * alpha + sum;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
         const float z[8] = {p[2 * y][0], p[2 * y][1], p[2 * y][2], p[2 * y][3],
                             p[2 * y + 1][0], p[2 * y + 1][1], p[2 * y + 1][2], p[2 * y + 1][3]};
         split_frag<NT>(pf[y], z);
     }
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) st.o[c] *= alpha;
     if constexpr (MASKED) {
         // Codes past every row's limit are whatever the page held: taken as
         // zeros.  A NaN below it, which some rows see and others do not, is
@@ -291,7 +303,7 @@ __device__ __forceinline__ void store_lse(const attn_args& a, int b, int h, int 
 
 // Few rows: WAVES waves take turns at the list's pages, each for all the rows.
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attn_cache_kernel(attn_args a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) {
     constexpr int NT = terms_of<T>, TR = TILE;
     __shared__ float so[WAVES][TR][D + 4];
     __shared__ float sml[WAVES][TR][2];
@@ -304,18 +316,22 @@ __global__ __launch_bounds__(64 * WAVES) void attn_cache_kernel(attn_args a) {
     const uint32_t bh = item / a.splits;
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
     const int r = tile * TR + col;
+    // a list in one piece starts at its first entry: fetched beside the lengths
+    uint64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < 64; i += WAVES) mine |= 1ull << i;
+    mine <<= wave;
+    const int32_t* list = list_of(a, b, h);
+    const int early = a.splits == 1 && lane < a.c.max_pages ? list[lane] : -1;
     const int limit = row_limit(a, b, r);
     const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(limit));
     const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(r < a.rows ? limit : INT32_MAX));
     const int pages = (lim_max + CACHE_TOKENS - 1) / CACHE_TOKENS;
     const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
-    uint64_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < 64; i += WAVES) mine |= 1ull << i;
-    mine <<= wave;
-    page_walk walk(list_of(a, b, h), lo, hi, a.c.pages);
-    if (lo < hi) walk.fetch(mine);
+    page_walk walk(list, lo, hi, a.c.pages);
+    if (a.splits == 1) walk.start(early, mine);
+    else if (lo < hi) walk.fetch(mine);
 
     frag_bf16 qf[D / 32][NT];
     const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
@@ -336,13 +352,12 @@ __global__ __launch_bounds__(64 * WAVES) void attn_cache_kernel(attn_args a) {
     for (int c = 0; c < D / 16; ++c) st.o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     const float scale = LOG2E / sqrtf(static_cast<float>(D));
     int pg, id;
-    while (walk.next(pg, id, mine)) {
-        const char* page = a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D);
-        if ((pg + 1) * CACHE_TOKENS <= lim_min)
-            page_step<T, D, false>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
-        else
-            page_step<T, D, true>(page, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
-    }
+    bool more = walk.next(pg, id, mine);
+    const auto page = [&]() { return a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D); };
+    for (; more && (pg + 1) * CACHE_TOKENS <= lim_min; more = walk.next(pg, id, mine))
+        page_step<T, D, false>(page(), 0, limit, lim_max, qf, scale, st);
+    for (; more; more = walk.next(pg, id, mine))
+        page_step<T, D, true>(page(), pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
     st.l += __shfl_xor(st.l, 16, 64);
     st.l += __shfl_xor(st.l, 32, 64);
 #pragma unroll

@@ -862,7 +862,7 @@ bool takes_tiles(int dtype, int64_t lists, int64_t rows) {
     return rows <= 64 || (rows <= 128 && (dtype == 0 || lists < 32));
 }
 
-attn_plan plan_attn(int dtype, const cache_view& c, int heads_q, int n) {
+attn_plan plan_attn(int dtype, int D, const cache_view& c, int heads_q, int n) {
     attn_plan p;
     const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n, heads = static_cast<int64_t>(c.batch) * c.heads;
     if (takes_tiles(dtype, heads, rows)) {
@@ -886,15 +886,17 @@ attn_plan plan_attn(int dtype, const cache_view& c, int heads_q, int n) {
     p.tile_rows = ROWS;
     p.waves = NW;
     p.tiles = (rows + ROWS - 1) / ROWS;
-    // Rounds of the 512 resident workgroups, against the one that evenly spread
-    // work would take; a split adds the partial results' way to memory and back,
-    // which measured 1% of a list of 36,000 tokens.
+    // Rounds of the resident workgroups (two a CU; one for fp32 at D = 128), against
+    // the one that evenly spread work would take; a split adds the partial results'
+    // way to memory and back, which measured 1% of a list of 36,000 tokens.
+    const int64_t resident = dtype == 0 && D == 128 ? 256 : 512;
     const int64_t items = heads * p.tiles, most = (c.max_pages + 7) / 8;
     double best = 0.;
     p.splits = 1;
-    for (int64_t k = 1; k <= most && (k == 1 || items * k <= 8 * 512); ++k) {
-        const int64_t rounds = (items * k + 511) / 512;
-        const double cost = static_cast<double>(rounds) / k + (k > 1 ? k * 360. / (64. * c.max_pages) * items / 512. : 0.);
+    for (int64_t k = 1; k <= most && (k == 1 || items * k <= 8 * resident); ++k) {
+        const int64_t rounds = (items * k + resident - 1) / resident;
+        const double cost = static_cast<double>(rounds) / k +
+                            (k > 1 ? k * 360. / (64. * c.max_pages) * items / resident : 0.);
         if (k == 1 || cost < best) {
             best = cost;
             p.splits = static_cast<int>(k);
@@ -908,7 +910,7 @@ attn_plan plan_attn(int dtype, const cache_view& c, int heads_q, int n) {
 size_t attn_cache_workspace_bytes(const cache_view& c, int D, int heads_q, int n) {
     size_t most = 0;
     for (int dtype = 0; dtype < 2; ++dtype) {
-        const attn_plan p = plan_attn(dtype, c, heads_q, n);
+        const attn_plan p = plan_attn(dtype, D, c, heads_q, n);
         const size_t need = p.splits == 1 ? 0 : static_cast<size_t>(c.batch) * c.heads * p.tiles * p.splits *
                                                     p.tile_rows * (D + 2) * sizeof(float);
         if (need > most) most = need;
@@ -937,7 +939,7 @@ void launch_attn(const attn_args& a, const attn_plan& p, hipStream_t s) {
 hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
                              const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
                              void* ws, hipStream_t s) {
-    const attn_plan p = plan_attn(dtype, c, heads_q, n);
+    const attn_plan p = plan_attn(dtype, D, c, heads_q, n);
     attn_args a{};
     a.c = c;
     a.q = q;

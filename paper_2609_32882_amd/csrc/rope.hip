@@ -419,7 +419,7 @@ __global__ __launch_bounds__(1024) void norm_rope_gain_kernel(const float* parti
 // Workgroups along the heads, so that a few tokens still fill the CUs.
 int head_split(int64_t groups, int heads) {
     const int64_t want = (1024 + groups - 1) / groups, most = (heads + ROPE_WAVES - 1) / ROPE_WAVES;
-    return static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+    return static_cast<int>(want > most ? most : want);
 }
 
 // Workgroups along the tokens in the gradients: each writes one partial row.

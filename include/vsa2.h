@@ -519,7 +519,8 @@ typedef struct {
  * Errors: NULL pointers; eps negative or not finite, a gain with eps = 0, a
  * pairing that is neither (VSA2_ERR_VALUE); an odd or negative axis, axes above
  * D, a table shorter than the grid, negative strides (VSA2_ERR_SHAPE);
- * misalignment; D not 64 or 128, more than 2^31 - 1 tokens (VSA2_ERR_UNSUPPORTED).
+ * misalignment; D not 64 or 128, tokens of all sequences (padding included) of
+ * 2^26 (D = 128) or 2^27 (D = 64) or more (VSA2_ERR_UNSUPPORTED).
  */
 vsa2_status vsa2_qk_norm_rope(const vsa2_problem* p, const vsa2_rope* r, float eps, const vsa2_rows* q_in,
                               const float* q_gain, void* q, const vsa2_rows* k_in, const float* k_gain, void* k,
@@ -593,7 +594,9 @@ vsa2_status vsa2_cache_page_bytes(int32_t head_dim, size_t* bytes);
  * vsa2_cache_read - the reverse: the same positions into rows of dtype; places
  *          past a count, outside the list or on a skipped page read as zeros.
  * Errors: NULL pointers, dtype, negative sizes or strides, D not 64 or 128,
- * table_heads neither 1 nor heads_kv, misalignment.  n = 0 does nothing.
+ * table_heads neither 1 nor heads_kv, misalignment; 2^24 or more pages' worth of
+ * a call's tokens over all sequences and KV heads (VSA2_ERR_UNSUPPORTED).  n = 0
+ * does nothing.
  */
 vsa2_status vsa2_cache_write(const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k, const vsa2_rows* v,
                              const int32_t* start, const int32_t* count, hipStream_t stream);
@@ -619,8 +622,12 @@ vsa2_status vsa2_cache_read(const vsa2_cache* c, int32_t dtype, int32_t n, const
  *   ws, ws_bytes  workspace of vsa2_attn_cache_workspace bytes, 256-byte aligned:
  *           partial results of long lists, which are split over workgroups and
  *           joined in a fixed order.
+ *   Sums are taken before the softmax's division, with weights of up to 2^8:
+ *   values times the list's length above 2^119 may overflow fp32 where their
+ *   mean would not.
  * Errors: as for vsa2_cache_write; heads_q not a multiple of heads_kv
- * (VSA2_ERR_SHAPE); workspace missing or too small.  n = 0 does nothing.
+ * (VSA2_ERR_SHAPE); 2^22 or more tiles of 16 rows over all sequences and KV heads
+ * (VSA2_ERR_UNSUPPORTED); workspace missing or too small.  n = 0 does nothing.
  */
 vsa2_status vsa2_attn_cache_workspace(const vsa2_cache* c, int32_t heads_q, int32_t n, size_t* bytes);
 vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n, const vsa2_rows* q,

@@ -641,7 +641,7 @@ class Rope:
         self.c = vsa2_rope()
         pairs = self.PAIRINGS[pairing]
         _marshal().fill_rope(self.c, axes, tables, origin, pairs)
-        self.tables, self.origin = tables, origin       # kept alive with their addresses
+        self.tables, self.origin = tuple(tables), origin       # kept alive with their addresses
 
 
 def _rope_c(rope, p):

@@ -141,6 +141,9 @@ vsa2::row_view view_of(const vsa2_rows* r) {
     return r ? vsa2::row_view{r->ptr, r->batch, r->head, r->token} : vsa2::row_view{nullptr, 0, 0, 0};
 }
 
+// A launch has fewer than 2^32 threads along an axis, 256 a workgroup.
+constexpr int64_t kMaxWorkgroups = (int64_t(1) << 24) - 1;
+
 // What norm and rotation check in both directions; fills the kernel's arguments.
 vsa2_status rope_setup(const vsa2_problem* p, const vsa2_rope* r, float eps, const float* q_gain, const float* k_gain,
                        shape* s, vsa2::rope_args* a) {
@@ -153,7 +156,8 @@ vsa2_status rope_setup(const vsa2_problem* p, const vsa2_rope* r, float eps, con
     a->grid = grid_of(p);
     a->Lj = s->Lj;
     a->eps = eps;
-    if (s->Lj > ((int64_t(1) << 31) - 1) / p->batch) return VSA2_ERR_UNSUPPORTED;
+    // a workgroup takes 512/D tokens
+    if (s->Lj > kMaxWorkgroups * (512 / p->head_dim) / p->batch) return VSA2_ERR_UNSUPPORTED;
     a->tokens = p->batch * s->Lj;
     a->part[0].gain = q_gain;
     a->part[1].gain = k_gain;
@@ -201,8 +205,6 @@ vsa2_status check_cache_memory(const vsa2_cache* c) {
     return VSA2_OK;
 }
 
-constexpr int64_t kMaxWorkgroups = (int64_t(1) << 31) - 1;
-
 vsa2_status cache_copy(bool write, const vsa2_cache* c, int32_t dtype, int32_t n, const vsa2_rows* k,
                        const vsa2_rows* v, const int32_t* start, const int32_t* count, hipStream_t stream) {
     vsa2::cache_view view;
@@ -228,7 +230,7 @@ vsa2_status check_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q
     // rows of a KV head, and workgroups of the unsplit launch
     const int64_t group = heads_q / c->heads_kv;
     if (group * n > (int64_t(1) << 30)) return VSA2_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(c->batch) * c->heads_kv > (int64_t(1) << 30) / (group * n / 16 + 1))
+    if (static_cast<int64_t>(c->batch) * c->heads_kv > kMaxWorkgroups / 4 / (group * n / 16 + 1))
         return VSA2_ERR_UNSUPPORTED;
     return VSA2_OK;
 }

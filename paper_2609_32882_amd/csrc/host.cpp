@@ -20,6 +20,7 @@
 namespace {
 
 PyObject* g_error = nullptr;      // raises the package's error for (function, status)
+thread_local int t_device = -1;   // the current GPU, on whose stream the call will run
 
 // A Python error is set; unwinds to the entry point.
 struct python_error {};
@@ -44,6 +45,12 @@ std::string shape_text(at::IntArrayRef s) {
          ") on " + t.device().str());
 }
 
+// A kernel of this GPU must not be handed another GPU's memory.
+void on_current_device(const at::Tensor& t, const char* name) {
+    if (t.device().index() != t_device)
+        fail(std::string(name) + ": on " + t.device().str() + ", but the current device is cuda:" + std::to_string(t_device));
+}
+
 // The tensor in a Python object; null for None.
 const at::Tensor* tensor(PyObject* o, const char* name) {
     if (o == Py_None) return nullptr;
@@ -61,6 +68,7 @@ P* contiguous(const at::Tensor* t, at::IntArrayRef shape, at::ScalarType dtype, 
     if (!t) return nullptr;
     if (t->sizes() != shape || t->scalar_type() != dtype || !t->is_cuda() || !t->is_contiguous())
         unexpected(name, *t, "contiguous", shape, dtype);
+    on_current_device(*t, name);
     return static_cast<P*>(t->data_ptr());
 }
 
@@ -68,6 +76,7 @@ P* contiguous(const at::Tensor* t, at::IntArrayRef shape, at::ScalarType dtype, 
 vsa2_rows rows(const at::Tensor& t, at::IntArrayRef shape, at::ScalarType dtype, const char* name) {
     if (t.sizes() != shape || t.scalar_type() != dtype || !t.is_cuda() || t.stride(3) != 1)
         unexpected(name, t, "rows of contiguous elements", shape, dtype);
+    on_current_device(t, name);
     return vsa2_rows{t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
 }
 
@@ -397,6 +406,7 @@ PyObject* set_error(PyObject* const* a, Py_ssize_t n) {
 // No exception leaves an entry point.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (hipGetDevice(&t_device) != hipSuccess) t_device = -1;      // without a GPU no tensor is on one
     try {
         return F(args, n);
     } catch (const python_error&) {

@@ -15,6 +15,8 @@
 // page is 16 KB in runs of 1 KB per load instruction; the waves of a workgroup
 // and the workgroups of a split take different pages of a list, each with its
 // own running maximum and sum, and are joined at the end in a fixed order.
+#include <algorithm>
+
 #include "common.hpp"
 
 namespace vsa2 {
@@ -24,7 +26,7 @@ namespace {
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.44269504088896340f;
-constexpr int TILE = 16;          // rows of a workgroup of attn_cache_kernel
+constexpr int TILE = 16;          // rows of a tile of attn_cache_kernel
 constexpr int NW = 4;             // waves of a workgroup of attn_cache_rows_kernel
 constexpr int ROWS = 32 * NW;     // its rows
 constexpr int STAGE = 2;          // pages it copies at a time
@@ -37,7 +39,8 @@ struct attn_args {
     const int32_t* count;
     float* part;         // [items][splits]: O [tile rows][D], then (m, l) [tile rows][2] of each
     int n, group, rows, tiles, splits;
-    bool causal;
+    uint32_t pieces;     // of all lists
+    bool causal, spread;
 };
 
 template <typename T> constexpr int terms_of = sizeof(T) == 4 ? 3 : 1;
@@ -162,6 +165,24 @@ struct page_walk {
     }
 };
 
+// The piece of a list, and its row tile, that a workgroup takes.  The tiles of a
+// piece run on one XCD, whose L2 then holds the piece's pages.  Spread: next pieces
+// on next XCDs, so that the long and the short sequences of a batch load all of
+// them alike (16 sequences of 20,000 to 76,800 tokens: 305 us against 332 with
+// neighbouring lists on one XCD, 16 x 8 lists of 200 rows 285 against 342); else a
+// run of pieces for every XCD, which keeps a few pieces of many tiles even (12 lists
+// of 1,792 rows: 444 us against 616 spread).
+__device__ __forceinline__ uint32_t piece_of(const attn_args& a, int& tile) {
+    if (!a.spread) {
+        const uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
+        tile = static_cast<int>(item % a.tiles);
+        return item / a.tiles;
+    }
+    const uint32_t turn = blockIdx.x >> 3, t = turn / a.tiles;
+    tile = static_cast<int>(turn - t * a.tiles);
+    return t * 8 + (blockIdx.x & 7);
+}
+
 __device__ __forceinline__ const int32_t* list_of(const attn_args& a, int b, int h) {
     return a.c.table + (static_cast<int64_t>(b) * a.c.table_heads + (a.c.table_heads > 1 ? h : 0)) * a.c.max_pages;
 }
@@ -174,81 +195,99 @@ struct tile_state {
     f32x4_t o[D / 16];
 };
 
-// One page for a tile.  MASKED: some row's limit, or the list's end, may lie
-// inside it.
-template <typename T, int D, bool MASKED>
-__device__ __forceinline__ void page_step(const char* page, int pos, int limit, int lim_max,
-                                          const frag_bf16 (&qf)[D / 32][terms_of<T>], float scale,
-                                          tile_state<D>& st) {
-    constexpr int NT = terms_of<T>;
-    const int lane = lane_id(), g = lane >> 4;
+// A lane's share of a page: K's codes of 16 t + lane % 16 and V's, and their powers.
+template <int D>
+struct page_data {
+    uint4 k[4 * (D / 64)], v[D / 16], ve;
+    uint32_t ke;
+};
+template <int D>
+__device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
+    const int lane = lane_id();
     const uint4* kp = reinterpret_cast<const uint4*>(page) + lane;
     const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
-    uint4 kr[4 * (D / 64)], vr[D / 16];
 #pragma unroll
-    for (int i = 0; i < 4 * (D / 64); ++i) kr[i] = kp[i * 64];
-    const uint32_t ke = *reinterpret_cast<const uint32_t*>(page + 128 * D + (lane & 15) * 4);
-    const uint4 ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + g * 16);
+    for (int i = 0; i < 4 * (D / 64); ++i) pd.k[i] = kp[i * 64];
+    pd.ke = *reinterpret_cast<const uint32_t*>(page + 128 * D + (lane & 15) * 4);
+    pd.ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + (lane >> 4) * 16);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) vr[i] = vp[i * 64];
+    for (int i = 0; i < D / 16; ++i) pd.v[i] = vp[i * 64];
+}
 
-    f32x4_t s[4];
+// One page for XT tiles, decoded once for all of them.  MASKED: some row's limit,
+// or the list's end, may lie inside it.
+template <typename T, int D, int XT, bool MASKED>
+__device__ __forceinline__ void page_step(const page_data<D>& pd, int pos, const int (&limit)[XT], int lim_max,
+                                          const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], float scale,
+                                          tile_state<D> (&st)[XT]) {
+    constexpr int NT = terms_of<T>;
+    const int g = lane_id() >> 4;
+    f32x4_t s[XT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const float power = power_of((ke >> (8 * t)) & 0xffu);
-        s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const float power = power_of((pd.ke >> (8 * t)) & 0xffu);
+#pragma unroll
+        for (int x = 0; x < XT; ++x) s[x][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < D / 64; ++u) {
-            const uint4 w = kr[t * (D / 64) + u];
+            const uint4 w = pd.k[t * (D / 64) + u];
             const frag_bf16 k0 = decode8(w.x, w.y, power), k1 = decode8(w.z, w.w, power);
 #pragma unroll
-            for (int y = NT - 1; y >= 0; --y) {
-                s[t] = mma16(k0, qf[2 * u][y], s[t]);
-                s[t] = mma16(k1, qf[2 * u + 1][y], s[t]);
-            }
+            for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+                for (int x = 0; x < XT; ++x) {
+                    s[x][t] = mma16(k0, qf[x][2 * u][y], s[x][t]);
+                    s[x][t] = mma16(k1, qf[x][2 * u + 1][y], s[x][t]);
+                }
         }
     }
-    const uint32_t vw[4] = {ve.x, ve.y, ve.z, ve.w};
-    if constexpr (MASKED) {
+    const uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
+    uint4 vr[D / 16];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) vr[c] = pd.v[c];
+    frag_bf16 pf[XT][2][NT];
+#pragma unroll
+    for (int x = 0; x < XT; ++x) {
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (pos + 16 * t + 4 * g + i >= limit[x]) s[x][t][i] = -INFINITY;
+        }
+        float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (pos + 16 * t + 4 * g + i >= limit) s[t][i] = -INFINITY;
-    }
-    float mx = -INFINITY;
+            for (int i = 0; i < 4; i += 2) mx = fmaxf(fmaxf(mx, s[x][t][i]), s[x][t][i + 1]);
+        mx = groups_max(mx) * scale;
+        // the running maximum moves only when it would grow by more than 8
+        // (weights up to 2^8 of the first): most pages leave O alone
+        if (__ballot(mx > st[x].m + 8.f) != 0) {
+            const float up = fmaxf(st[x].m, mx);
+            const float f = up == -INFINITY ? 1.f : fast_exp2(st[x].m - up);
+            st[x].m = up;
+            st[x].l *= f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
-    mx = groups_max(mx) * scale;
-    // the running maximum moves only when it would grow by more than 8
-    // (weights up to 2^8 of the first): most pages leave O alone
-    if (__ballot(mx > st.m + 8.f) != 0) {
-        const float up = fmaxf(st.m, mx);
-        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
-        st.m = up;
-        st.l *= f;
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) st.o[c] *= f;
-    }
-    const float base = st.m == -INFINITY ? 0.f : st.m;
-    frag_bf16 pf[2][NT];
-    float p[4][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float e = fast_exp2(fmaf(s[t][i], scale, -base));
-            st.l += e;
-            // a masked place's power may be anything
-            p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
+            for (int c = 0; c < D / 16; ++c) st[x].o[c] *= f;
         }
+        const float base = st[x].m == -INFINITY ? 0.f : st[x].m;
+        float p[4][4];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-        const float z[8] = {p[2 * y][0], p[2 * y][1], p[2 * y][2], p[2 * y][3],
-                            p[2 * y + 1][0], p[2 * y + 1][1], p[2 * y + 1][2], p[2 * y + 1][3]};
-        split_frag<NT>(pf[y], z);
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = fast_exp2(fmaf(s[x][t][i], scale, -base));
+                st[x].l += e;
+                // a masked place's power may be anything
+                p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
+            }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const float z[8] = {p[2 * y][0], p[2 * y][1], p[2 * y][2], p[2 * y][3],
+                                p[2 * y + 1][0], p[2 * y + 1][1], p[2 * y + 1][2], p[2 * y + 1][3]};
+            split_frag<NT>(pf[x][y], z);
+        }
     }
     if constexpr (MASKED) {
         // Codes past every row's limit are whatever the page held: taken as
@@ -271,12 +310,15 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
             }
             vr[c] = make_uint4(w[0], w[1], w[2], w[3]);
             if (__ballot((nan[0] | nan[1] | nan[2] | nan[3]) != 0) != 0) {
-                f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                hit = mma16(decode8(nan[0] & ONE_E4M3, nan[1] & ONE_E4M3, 1.f), pf[0][0], hit);
-                hit = mma16(decode8(nan[2] & ONE_E4M3, nan[3] & ONE_E4M3, 1.f), pf[1][0], hit);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
+                for (int x = 0; x < XT; ++x) {
+                    f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    hit = mma16(decode8(nan[0] & ONE_E4M3, nan[1] & ONE_E4M3, 1.f), pf[x][0][0], hit);
+                    hit = mma16(decode8(nan[2] & ONE_E4M3, nan[3] & ONE_E4M3, 1.f), pf[x][1][0], hit);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(hit[i] == 0.f)) st[x].o[c][i] = __uint_as_float(0x7fc00000u);
+                }
             }
         }
     }
@@ -284,10 +326,12 @@ __device__ __forceinline__ void page_step(const char* page, int pos, int limit, 
     for (int c = 0; c < D / 16; ++c) {
         const frag_bf16 v0 = decode8(vr[c].x, vr[c].y, 1.f), v1 = decode8(vr[c].z, vr[c].w, 1.f);
 #pragma unroll
-        for (int y = NT - 1; y >= 0; --y) {
-            st.o[c] = mma16(v0, pf[0][y], st.o[c]);
-            st.o[c] = mma16(v1, pf[1][y], st.o[c]);
-        }
+        for (int y = NT - 1; y >= 0; --y)
+#pragma unroll
+            for (int x = 0; x < XT; ++x) {
+                st[x].o[c] = mma16(v0, pf[x][0][y], st[x].o[c]);
+                st[x].o[c] = mma16(v1, pf[x][1][y], st[x].o[c]);
+            }
     }
 }
 
@@ -301,21 +345,20 @@ __device__ __forceinline__ void store_lse(const attn_args& a, int b, int h, int 
     a.lse[(static_cast<int64_t>(b) * a.c.heads * a.group + h * a.group + hg) * a.n + i] = (base + log2f(l)) * LN2;
 }
 
-// Few rows: WAVES waves take turns at the list's pages, each for all the rows.
-template <typename T, int D, int WAVES>
+// Few rows: WAVES waves take turns at the list's pages, each for all the rows
+// (XT tiles of 16).
+template <typename T, int D, int WAVES, int XT>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) {
-    constexpr int NT = terms_of<T>, TR = TILE;
+    constexpr int NT = terms_of<T>, TR = XT * TILE;
     __shared__ float so[WAVES][TR][D + 4];
     __shared__ float sml[WAVES][TR][2];
     const int lane = lane_id(), wave = wave_id(), g = lane >> 4, col = lane & 15;
-    // row tiles of a list's piece share its pages: next to each other on one XCD
-    uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
-    const int tile = static_cast<int>(item % a.tiles);
-    item /= a.tiles;
+    int tile;
+    const uint32_t item = piece_of(a, tile);
+    if (item >= a.pieces) return;
     const int split = static_cast<int>(item % a.splits);
     const uint32_t bh = item / a.splits;
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
-    const int r = tile * TR + col;
     // a list in one piece starts at its first entry: fetched beside the lengths
     uint64_t mine = 0;
 #pragma unroll
@@ -323,9 +366,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) 
     mine <<= wave;
     const int32_t* list = list_of(a, b, h);
     const int early = a.splits == 1 && lane < a.c.max_pages ? list[lane] : -1;
-    const int limit = row_limit(a, b, r);
-    const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(limit));
-    const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(r < a.rows ? limit : INT32_MAX));
+    // rows that see nothing take what the others compute and drop it at the end
+    int limit[XT], most = 0, least = INT32_MAX;
+#pragma unroll
+    for (int x = 0; x < XT; ++x) {
+        limit[x] = row_limit(a, b, tile * TR + x * TILE + col);
+        most = max(most, limit[x]);
+        least = limit[x] > 0 ? min(least, limit[x]) : least;
+    }
+    const int lim_max = __builtin_amdgcn_readfirstlane(lanes_max(most));
+    const int lim_min = __builtin_amdgcn_readfirstlane(lanes_min(least));
     const int pages = (lim_max + CACHE_TOKENS - 1) / CACHE_TOKENS;
     const int lo = static_cast<int>(static_cast<int64_t>(pages) * split / a.splits);
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
@@ -333,44 +383,62 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) 
     if (a.splits == 1) walk.start(early, mine);
     else if (lo < hi) walk.fetch(mine);
 
-    frag_bf16 qf[D / 32][NT];
-    const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
+    frag_bf16 qf[XT][D / 32][NT];
+    tile_state<D> st[XT];
 #pragma unroll
-    for (int u = 0; u < D / 32; ++u) {
-        float y[8] = {};
-        if (r < a.rows) {
-            const T* e = q + (u / 2) * 64 + g * 16 + (u & 1) * 8;
+    for (int x = 0; x < XT; ++x) {
+        const int r = tile * TR + x * TILE + col;
+        const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset(a.q, a, b, h, r) : 0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
+        for (int u = 0; u < D / 32; ++u) {
+            float y[8] = {};
+            if (r < a.rows) {
+                const T* e = q + (u / 2) * 64 + g * 16 + (u & 1) * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
+            }
+            split_frag<NT>(qf[x][u], y);
         }
-        split_frag<NT>(qf[u], y);
-    }
-    tile_state<D> st;
-    st.m = -INFINITY;
-    st.l = 0.f;
+        st[x].m = -INFINITY;
+        st[x].l = 0.f;
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) st.o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < D / 16; ++c) st[x].o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
     const float scale = LOG2E / sqrtf(static_cast<float>(D));
     int pg, id;
     bool more = walk.next(pg, id, mine);
     const auto page = [&]() { return a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D); };
-    for (; more && (pg + 1) * CACHE_TOKENS <= lim_min; more = walk.next(pg, id, mine))
-        page_step<T, D, false>(page(), 0, limit, lim_max, qf, scale, st);
-    for (; more; more = walk.next(pg, id, mine))
-        page_step<T, D, true>(page(), pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
-    st.l += __shfl_xor(st.l, 16, 64);
-    st.l += __shfl_xor(st.l, 32, 64);
+    const auto whole = [&]() { return more && (pg + 1) * CACHE_TOKENS <= lim_min; };
+    for (; whole(); more = walk.next(pg, id, mine)) {
+        page_data<D> x;
+        load_page<D>(x, page());
+        page_step<T, D, XT, false>(x, 0, limit, lim_max, qf, scale, st);
+    }
+    for (; more; more = walk.next(pg, id, mine)) {
+        page_data<D> x;
+        load_page<D>(x, page());
+        page_step<T, D, XT, true>(x, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+    }
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) *reinterpret_cast<f32x4_t*>(&so[wave][col][16 * c + 4 * g]) = st.o[c];
-    if (g == 0) {
-        sml[wave][col][0] = st.m;
-        sml[wave][col][1] = st.l;
+    for (int x = 0; x < XT; ++x) {
+        float l = st[x].l;
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        const bool dead = limit[x] == 0;
+        const int row = x * TILE + col;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+            *reinterpret_cast<f32x4_t*>(&so[wave][row][16 * c + 4 * g]) = dead ? f32x4_t{0.f, 0.f, 0.f, 0.f} : st[x].o[c];
+        if (g == 0) {
+            sml[wave][row][0] = dead ? -INFINITY : st[x].m;
+            sml[wave][row][1] = dead ? 0.f : l;
+        }
     }
     __syncthreads();
     // join the waves: a thread takes 4 elements of a row
     for (int at = threadIdx.x; at < TR * (D / 4); at += 64 * WAVES) {
         const int row = at / (D / 4), d0 = at % (D / 4) * 4, rr = tile * TR + row;
-        if (rr >= a.rows && a.splits == 1) continue;
+        if (rr >= a.rows) continue;
         float m = sml[0][row][0];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sml[w][row][0]);
@@ -632,16 +700,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     __shared__ __attribute__((aligned(1024))) char codes[2][STAGE][128 * D];
     __shared__ __attribute__((aligned(16))) float power[NW][STAGE][2][64];
     const int lane = lane_id(), wave = wave_id(), h2 = lane >> 5, col = lane & 31;
-    uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
-    const int tile = static_cast<int>(item % a.tiles);
-    item /= a.tiles;
+    int tile;
+    const uint32_t item = piece_of(a, tile);
+    if (item >= a.pieces) return;
     const int split = static_cast<int>(item % a.splits);
     const uint32_t bh = item / a.splits;
     const int b = static_cast<int>(bh / a.c.heads), h = static_cast<int>(bh % a.c.heads);
     const int r = tile * ROWS + wave * 32 + col;
     const int limit = row_limit(a, b, r);
-    // the rows' limits: the wave's largest, the workgroup's largest and (of rows that exist) smallest
-    int wmax = limit, wmin = r < a.rows ? limit : INT32_MAX;
+    // the rows' limits: the wave's largest, the workgroup's largest and (of rows that see something,
+    // the others drop what they compute at the end) smallest
+    int wmax = limit, wmin = limit > 0 ? limit : INT32_MAX;
 #pragma unroll
     for (int m = 16; m; m >>= 1) {
         wmin = min(wmin, __shfl_xor(wmin, m, 64));
@@ -744,11 +813,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
         }
         buf ^= 1;
     }
-    const float m = st.m;
-    float l = st.l;
     f32x16_t(&o)[VC] = st.o;
+    float m = st.m, l = st.l;
     l += swap_half(l);
+    if (limit == 0) {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    }
     const float base = m == -INFINITY ? 0.f : m;
+    if (r >= a.rows) return;
     if (a.splits > 1) {
         float* part = a.part + ((static_cast<int64_t>(bh) * a.tiles + tile) * a.splits + split) * (ROWS * (D + 2));
         const int row = wave * 32 + col;
@@ -765,7 +842,6 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
         }
         return;
     }
-    if (r >= a.rows) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* out = static_cast<T*>(a.o.ptr) + row_offset(a.o, a, b, h, r);
 #pragma unroll
@@ -782,11 +858,12 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
 
 // Joins the pieces of a row tile.  A row is joined by SLICES groups of 32 lanes,
 // each taking every SLICES-th piece, whose sums are added in order: one group
-// (8 rows a workgroup) for up to 8 pieces, eight groups for more, where one
-// group's loads one after the other took longer than the pieces themselves.
+// (8 rows a workgroup) for up to 8 pieces, eight groups for up to 32, 32 for more,
+// where a group's loads one after the other took longer than the pieces themselves
+// (512 pieces of one row: the whole call 40.5 us with eight groups, 28.5 with 32).
 template <typename T, int D, int SLICES>
-__global__ __launch_bounds__(256) void attn_cache_join_kernel(attn_args a, int tile_rows) {
-    constexpr int RPW = 8 / SLICES;       // rows of a workgroup
+__global__ __launch_bounds__(SLICES > 8 ? 32 * SLICES : 256) void attn_cache_join_kernel(attn_args a, int tile_rows) {
+    constexpr int RPW = SLICES > 8 ? 1 : 8 / SLICES;       // rows of a workgroup
     __shared__ float so[SLICES > 1 ? SLICES : 1][D], sl[SLICES];
     const int64_t stride = static_cast<int64_t>(tile_rows) * (D + 2);
     const int subs = tile_rows / RPW;
@@ -851,36 +928,62 @@ struct attn_plan {
     int splits;
 };
 
-// Which kernel: 16-row tiles whose waves share out a list's pages, or 128-row
-// tiles whose waves share the pages.  The first reads a page once per 16 rows
-// but splits finely; measured over lists of 20,000 tokens, D = 128 (us, 16-row
-// against 128-row tiles): bf16, 8 lists of 128 rows 34 against 44, 16 of 80
-// rows 45 against 52, 32 of 80 rows 77 against 73, of 128 rows 99 against 76,
-// 128 lists of 32, 64 and 128 rows 137 / 203 / 342 against 154 / 202 / 224;
-// fp32, 128 lists of 64, 96 and 128 rows 287 / 407 / 511 against 432 / 471 / 508.
-bool takes_tiles(int dtype, int64_t lists, int64_t rows) {
-    return rows <= 64 || (rows <= 128 && (dtype == 0 || lists < 32));
+// fp32 rows of D = 128 take three times the registers: a pair of tiles would not fit.
+template <typename T, int D> constexpr bool two_tiles = !(sizeof(T) == 4 && D == 128);
+
+// Which kernel: tiles of 16 or 32 rows whose waves share out a list's pages, or
+// 128-row tiles whose waves share the pages.  The first reads and decodes a page
+// once per tile but splits finely; measured over lists of 20,000 tokens (us,
+// small tiles against 128-row ones): bf16, D = 128, 8 lists of 128 rows 27 against
+// 36, 32 of 128 rows 63 against 66, 128 lists of 64 rows 162 against 196, of 96
+// rows 229 against 209; fp32, D = 128, 32 lists of 128 rows 124 against 124.
+bool takes_tiles(int dtype, int D, int64_t lists, int64_t rows) {
+    return rows <= 64 || (rows <= 128 && ((dtype == 0 && D == 128) || lists < 64));
+}
+
+// Small tiles of 32 rows: half the decoding, where there are workgroups enough
+// either way.  Measured with 128 lists (us, 16 rows against 32): lists of 40,000
+// tokens, bf16, D = 128, 32 / 48 / 64 rows 247 / 346 / 382 against 246 / 290 / 308;
+// D = 64 136 / 169 / 206 against 133 / 187 / 190 (a half-empty pair costs more than
+// it saves there); 5,000 tokens 27 / 32 / 33 against 30 / 33 / 34.  Of short
+// lists, where a pair makes the tiles one and the call one launch: 32 rows of 1,000
+// tokens 16.6 against 14.6.
+bool takes_pairs(int dtype, int D, int64_t lists, int64_t rows, int pages) {
+    const int64_t tiles = (rows + TILE - 1) / TILE;
+    if (tiles == 1 || (dtype == 0 && D == 128) || lists * tiles < 128) return false;
+    if (pages <= 32) return tiles == 2;
+    return pages >= 128 && (tiles % 2 == 0 || (dtype == 1 && D == 128));
 }
 
 attn_plan plan_attn(int dtype, int D, const cache_view& c, int heads_q, int n) {
     attn_plan p;
-    const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n, heads = static_cast<int64_t>(c.batch) * c.heads;
-    if (takes_tiles(dtype, heads, rows)) {
-        p.tile_rows = TILE;
-        p.tiles = (rows + TILE - 1) / TILE;
-        // A short list stays in one piece, whose eight waves join it without a
-        // second launch; else the 512 workgroups of four waves that are resident
-        // at once (D = 128), and a page for every wave at least.  One token over
-        // 200,000: 1,024 workgroups 118 us, 512 85 (join included), 256 82; 20
-        // rows of 8 lists of 30,000 tokens 107 / 101 / 107.
-        if (p.tiles == 1 && c.max_pages <= 32) {
+    const int64_t rows = static_cast<int64_t>(heads_q / c.heads) * n, lists = static_cast<int64_t>(c.batch) * c.heads;
+    if (takes_tiles(dtype, D, lists, rows)) {
+        p.tile_rows = takes_pairs(dtype, D, lists, rows, c.max_pages) ? 2 * TILE : TILE;
+        p.tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+        // A list in one piece takes eight waves that join it without a second
+        // launch: short ones, and those of many sequences up to 200 pages.  One
+        // token, in one piece against several (us): 12 lists of 1,792 tokens, bf16
+        // 10.5 against 10.9, fp32 (D = 128) 13.7 against 11.4; 128 lists of 4,000,
+        // bf16 24.5 against 29.5, fp32 30.0 against 29.4; 192 of 6,000, bf16 47
+        // against 54, fp32 51 against 55.
+        const int one = lists >= (dtype == 1 ? 128 : 192) ? 200 : (dtype == 0 && D == 128 && lists < 128 ? 16 : 32);
+        if (p.tiles == 1 && c.max_pages <= one) {
             p.waves = 8;
             p.splits = 1;
             return p;
         }
+        // Else the 512 workgroups of four waves that are resident at once (D = 128),
+        // and a page for every wave at least; 256 where the pieces of few rows take
+        // longer to join than they save (one token over 200,000: 512 workgroups 28
+        // us, 256 22); 1,024 where many sequences are of different lengths and the
+        // pieces stay long (16 x 8 lists of 20,000 to 76,800 tokens: 512 workgroups
+        // 305 us, 1,024 286, 2,048 336).
         p.waves = 4;
-        const int64_t want = 512 / (heads * p.tiles), most = (c.max_pages + 3) / 4;
-        p.splits = static_cast<int>(want < 1 ? 1 : (want > most ? most : want));
+        const int64_t items = lists * p.tiles, most = (c.max_pages + 3) / 4, pages64 = c.max_pages / 64;
+        int64_t want = (dtype == 1 && p.tiles == 1 && items <= 16 ? 256 : 512) / items;
+        if (items >= 128) want = std::max(want, std::min(1024 / items, pages64));
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
         return p;
     }
     p.tile_rows = ROWS;
@@ -890,7 +993,7 @@ attn_plan plan_attn(int dtype, int D, const cache_view& c, int heads_q, int n) {
     // the one that evenly spread work would take; a split adds the partial results'
     // way to memory and back, which measured 1% of a list of 36,000 tokens.
     const int64_t resident = dtype == 0 && D == 128 ? 256 : 512;
-    const int64_t items = heads * p.tiles, most = (c.max_pages + 7) / 8;
+    const int64_t items = lists * p.tiles, most = (c.max_pages + 7) / 8;
     double best = 0.;
     p.splits = 1;
     for (int64_t k = 1; k <= most && (k == 1 || items * k <= 8 * resident); ++k) {
@@ -923,12 +1026,20 @@ namespace {
 template <typename T, int D>
 void launch_attn(const attn_args& a, const attn_plan& p, hipStream_t s) {
     const int64_t items = static_cast<int64_t>(a.c.batch) * a.c.heads * p.tiles;
-    const dim3 grid(static_cast<unsigned>(items * p.splits)), block(64 * p.waves);
+    const int64_t pieces = a.spread ? (static_cast<int64_t>(a.pieces) + 7) / 8 * 8 : a.pieces;
+    const dim3 grid(static_cast<unsigned>(pieces * p.tiles)), block(64 * p.waves);
     if (p.tile_rows == ROWS) hipLaunchKernelGGL((attn_cache_rows_kernel<T, D>), grid, block, 0, s, a);
-    else if (p.waves == 8) hipLaunchKernelGGL((attn_cache_kernel<T, D, 8>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((attn_cache_kernel<T, D, 4>), grid, block, 0, s, a);
+    else if (p.tile_rows == TILE) {
+        if (p.waves == 8) hipLaunchKernelGGL((attn_cache_kernel<T, D, 8, 1>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((attn_cache_kernel<T, D, 4, 1>), grid, block, 0, s, a);
+    } else if constexpr (two_tiles<T, D>) {
+        if (p.waves == 8) hipLaunchKernelGGL((attn_cache_kernel<T, D, 8, 2>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((attn_cache_kernel<T, D, 4, 2>), grid, block, 0, s, a);
+    }
     const auto rows_of = [&](int per_wg) { return dim3(static_cast<unsigned>(items * (p.tile_rows / per_wg))); };
-    if (p.splits > 8)
+    if (p.splits > 32)
+        hipLaunchKernelGGL((attn_cache_join_kernel<T, D, 32>), rows_of(1), dim3(1024), 0, s, a, p.tile_rows);
+    else if (p.splits > 8)
         hipLaunchKernelGGL((attn_cache_join_kernel<T, D, 8>), rows_of(1), dim3(256), 0, s, a, p.tile_rows);
     else if (p.splits > 1)
         hipLaunchKernelGGL((attn_cache_join_kernel<T, D, 1>), rows_of(8), dim3(256), 0, s, a, p.tile_rows);
@@ -954,6 +1065,8 @@ hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q,
     a.tiles = static_cast<int>(p.tiles);
     a.splits = p.splits;
     a.causal = causal;
+    a.pieces = static_cast<uint32_t>(static_cast<int64_t>(c.batch) * c.heads * p.splits);
+    a.spread = p.tile_rows != ROWS || a.pieces >= 128;
     if (dtype == 0 && D == 64) launch_attn<float, 64>(a, p, s);
     else if (dtype == 0) launch_attn<float, 128>(a, p, s);
     else if (D == 64) launch_attn<bf16_t, 64>(a, p, s);

@@ -1,7 +1,7 @@
 // Attention of new tokens over the paged 8-bit cache.
 //
 // Rows: the query heads of one KV head times the call's tokens (token-major), in
-// tiles of 16.  Everything is computed transposed, S^T = K Q^T and
+// tiles of 16 (or pairs of them, or 128).  Everything is computed transposed, S^T = K Q^T and
 // O^T = V^T P^T on 16x16x32 bf16 MFMAs, so that a lane holds one row (column
 // lane % 16) through the whole kernel: the softmax needs two exchanges a page,
 // P goes from the accumulators of the first product into the operand of the
@@ -14,7 +14,10 @@
 // Bound by memory for single tokens: 2 (D + 1) bytes per token and KV head.  A
 // page is 16 KB in runs of 1 KB per load instruction; the waves of a workgroup
 // and the workgroups of a split take different pages of a list, each with its
-// own running maximum and sum, and are joined at the end in a fixed order.
+// own running maximum and sum, and are joined at the end in a fixed order.  16
+// sequences of 20,000 to 76,800 tokens, 40 query and 8 KV heads of 128: 281 us, 5.7
+// TB/s.  Bound by issue for many rows: 1,792 tokens over 35,840, 12 heads, 410 us,
+// 0.96 PFLOP/s.
 #include <algorithm>
 
 #include "common.hpp"
@@ -45,7 +48,9 @@ struct attn_args {
 
 template <typename T> constexpr int terms_of = sizeof(T) == 4 ? 3 : 1;
 
-// 8 values as the sum of bf16 fragments (one, or three for fp32: 24 bits).
+// 8 values as the sum of bf16 fragments: three for fp32 (24 bits); one for bf16, where
+// queries are exact and probabilities rounded to 8 bits, an error below the rounding of
+// the inputs themselves (the sum of the weights keeps 32).
 template <int N>
 __device__ __forceinline__ void split_frag(frag_bf16* f, const float* x) {
     if constexpr (N == 1) {

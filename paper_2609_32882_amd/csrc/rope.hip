@@ -8,7 +8,9 @@
 // piece).  What depends on the token alone (its place, its sequence, its 4
 // (cos, sin) pairs) is worked out once per lane and kept while the wave walks
 // over the heads; neighbouring waves take neighbouring heads, whose input rows
-// lie side by side in a projection.
+// lie side by side in a projection.  A 20x48x80 grid with 40 + 40 + 40 heads of
+// 128 in bf16 takes 930 us (5.0 TB/s, a large copy's rate); its gradients with
+// 12 + 12 + 12 heads 375 us (5.0 TB/s).
 #include "common.hpp"
 
 namespace vsa2 {
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(64 * ROPE_WAVES) void norm_rope_bwd_kernel(rope_arg
     const int64_t groups = (a.tokens + RPW - 1) / RPW;
     for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
         const lane_token t = find_token<HALVES>(a, group * RPW + rr, c);
-        constexpr int AHEAD = 2;
+        constexpr int AHEAD = 2;       // three or four: fp32 255 -> 305 us (20x48x40, 8 heads), bf16 the same
         for (int h0 = slot; h0 < heads; h0 += stride * AHEAD) {
             raw8<T> rg[AHEAD], rx[AHEAD];
 #pragma unroll

@@ -89,6 +89,12 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
     return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
 }
 constexpr uint32_t ONE_E4M3 = 0x38383838u;     // four codes of 1.0
+// 0xff in the first n of four bytes.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : ~0u >> (32 - 8 * n)); }
+// Ones for the first a of four tokens and the first b of four more.
+__device__ __forceinline__ frag_bf16 shown8(int a, int b) {
+    return decode8(first_bytes(a) & ONE_E4M3, first_bytes(b) & ONE_E4M3, 1.f);
+}
 
 __device__ __forceinline__ void store4(float* p, const float* x) {
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
@@ -222,7 +228,7 @@ __device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
 // One page for XT tiles, decoded once for all of them.  MASKED: some row's limit,
 // or the list's end, may lie inside it.
 template <typename T, int D, int XT, bool MASKED>
-__device__ __forceinline__ void page_step(const page_data<D>& pd, int pos, const int (&limit)[XT], int lim_max,
+__device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos, const int (&limit)[XT], int lim_max,
                                           const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], float scale,
                                           tile_state<D> (&st)[XT]) {
     constexpr int NT = terms_of<T>;
@@ -294,37 +300,23 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, int pos, const
             split_frag<NT>(pf[x][y], z);
         }
     }
+    uint32_t keep[4], any = 0;
     if constexpr (MASKED) {
         // Codes past every row's limit are whatever the page held: taken as
         // zeros.  A NaN below it, which some rows see and others do not, is
-        // taken out of the product and given to the rows that see it (a second
-        // product counts their weight on it).
-        uint32_t keep[4];
+        // taken out of the product, too.
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int left = lim_max - (pos + 16 * t + 4 * g);
-            keep[t] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
-        }
+        for (int t = 0; t < 4; ++t) keep[t] = first_bytes(lim_max - (pos + 16 * t + 4 * g));
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-            uint32_t w[4] = {vr[c].x & keep[0], vr[c].y & keep[1], vr[c].z & keep[2], vr[c].w & keep[3]}, nan[4];
+            uint32_t w[4] = {vr[c].x & keep[0], vr[c].y & keep[1], vr[c].z & keep[2], vr[c].w & keep[3]};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                nan[t] = nan_bytes(w[t]);
-                w[t] &= ~nan[t];
+                const uint32_t nan = nan_bytes(w[t]);
+                w[t] &= ~nan;
+                any |= nan;
             }
             vr[c] = make_uint4(w[0], w[1], w[2], w[3]);
-            if (__ballot((nan[0] | nan[1] | nan[2] | nan[3]) != 0) != 0) {
-#pragma unroll
-                for (int x = 0; x < XT; ++x) {
-                    f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
-                    hit = mma16(decode8(nan[0] & ONE_E4M3, nan[1] & ONE_E4M3, 1.f), pf[x][0][0], hit);
-                    hit = mma16(decode8(nan[2] & ONE_E4M3, nan[3] & ONE_E4M3, 1.f), pf[x][1][0], hit);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!(hit[i] == 0.f)) st[x].o[c][i] = __uint_as_float(0x7fc00000u);
-                }
-            }
         }
     }
 #pragma unroll
@@ -337,6 +329,30 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, int pos, const
                 st[x].o[c] = mma16(v0, pf[x][0][y], st[x].o[c]);
                 st[x].o[c] = mma16(v1, pf[x][1][y], st[x].o[c]);
             }
+    }
+    if constexpr (MASKED) {
+        // A NaN goes to the rows that see it, whatever their weight on it: a second product,
+        // from the page's codes once more, counts it where a row's limit lies past it.
+        if (__ballot(any != 0) == 0) return;
+        const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane_id();
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+            const uint4 v = vp[c * 64];
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t nan[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) nan[t] = nan_bytes(w[t] & keep[t]) & ONE_E4M3;
+#pragma unroll
+            for (int x = 0; x < XT; ++x) {
+                const int here = limit[x] - (pos + 4 * g);
+                f32x4_t hit = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                hit = mma16(decode8(nan[0], nan[1], 1.f), shown8(here, here - 16), hit);
+                hit = mma16(decode8(nan[2], nan[3], 1.f), shown8(here - 32, here - 48), hit);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (hit[i] != 0.f) st[x].o[c][i] = __uint_as_float(0x7fc00000u);
+            }
+        }
     }
 }
 
@@ -417,12 +433,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) 
     for (; whole(); more = walk.next(pg, id, mine)) {
         page_data<D> x;
         load_page<D>(x, page());
-        page_step<T, D, XT, false>(x, 0, limit, lim_max, qf, scale, st);
+        page_step<T, D, XT, false>(x, nullptr, 0, limit, lim_max, qf, scale, st);
     }
     for (; more; more = walk.next(pg, id, mine)) {
         page_data<D> x;
         load_page<D>(x, page());
-        page_step<T, D, XT, true>(x, pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+        page_step<T, D, XT, true>(x, page(), pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
     }
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
@@ -576,47 +592,49 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
         }
         split_frag<NT>(pf[t], y);
     }
-    uint32_t keep[4][2];
+    uint32_t keep[4][2], any = 0;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const int left = wmax - (first + 16 * t + 8 * x + 4 * h2);
-            keep[t][x] = left >= 4 ? ~0u : (left <= 0 ? 0u : ~0u >> (32 - 8 * left));
-        }
+        for (int x = 0; x < 2; ++x) keep[t][x] = first_bytes(wmax - (first + 16 * t + 8 * x + 4 * h2));
+    // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
 #pragma unroll
     for (int c = 0; c < VC; ++c) {
         const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
         const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
         uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
-        // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
-        uint32_t nan[4][2], any = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 w[t][x] &= keep[t][x];
-                nan[t][x] = nan_bytes(w[t][x]);
-                w[t][x] &= ~nan[t][x];
-                any |= nan[t][x];
+                const uint32_t nan = nan_bytes(w[t][x]);
+                w[t][x] &= ~nan;
+                any |= nan;
             }
-        if (__ballot(any != 0) != 0) {
-            f32x16_t hit;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) hit[i] = 0.f;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                mma(hit, decode8(nan[t][0] & ONE_E4M3, nan[t][1] & ONE_E4M3, 1.f), pf[t][0]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!(hit[i] == 0.f)) st.o[c][i] = __uint_as_float(0x7fc00000u);
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
             const frag_bf16 vf = decode8(w[t][0], w[t][1], 1.f);
 #pragma unroll
             for (int z = NT - 1; z >= 0; --z) mma(st.o[c], vf, pf[t][z]);
         }
+    }
+    if (__ballot(any != 0) == 0) return;
+#pragma unroll
+    for (int c = 0; c < VC; ++c) {
+        const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
+        const uint4 vb = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512);
+        const uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
+        f32x16_t hit;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int here = limit - (first + 16 * t + 4 * h2);
+            mma(hit, decode8(nan_bytes(w[t][0] & keep[t][0]) & ONE_E4M3, nan_bytes(w[t][1] & keep[t][1]) & ONE_E4M3, 1.f),
+                shown8(here, here - 8));
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (hit[i] != 0.f) st.o[c][i] = __uint_as_float(0x7fc00000u);
     }
 }
 

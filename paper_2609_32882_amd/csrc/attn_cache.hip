@@ -19,6 +19,7 @@
 // TB/s.  Bound by issue for many rows: 1,792 tokens over 35,840, 12 heads, 410 us,
 // 0.96 PFLOP/s.
 #include <algorithm>
+#include <cfloat>
 
 #include "common.hpp"
 
@@ -89,6 +90,11 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
     return ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
 }
 constexpr uint32_t ONE_E4M3 = 0x38383838u;     // four codes of 1.0
+// NaN for a count above zero, else 0 (by arithmetic: as many masks as there are counts would not
+// fit the scalar registers).
+__device__ __forceinline__ float nan_if(float count) {
+    return count * FLT_MAX * FLT_MAX * 0.f;         // an infinity, or 0, times 0
+}
 // 0xff in the first n of four bytes.
 __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (n <= 0 ? 0u : ~0u >> (32 - 8 * n)); }
 // Ones for the first a of four tokens and the first b of four more.
@@ -350,7 +356,7 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
                 hit = mma16(decode8(nan[2], nan[3], 1.f), shown8(here - 32, here - 48), hit);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (hit[i] != 0.f) st[x].o[c][i] = __uint_as_float(0x7fc00000u);
+                    st[x].o[c][i] += nan_if(hit[i]);
             }
         }
     }
@@ -367,9 +373,12 @@ __device__ __forceinline__ void store_lse(const attn_args& a, int b, int h, int 
 }
 
 // Few rows: WAVES waves take turns at the list's pages, each for all the rows
-// (XT tiles of 16).
+// (XT tiles of 16).  Two waves a SIMD at D = 128, also where the registers would hold
+// three: plan_attn cuts lists for that (16 x 8 lists of 20,000 to 76,800 tokens: 280 us
+// against 290).
 template <typename T, int D, int WAVES, int XT>
-__global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(attn_args a) {
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D == 128 ? 2 : 4))) void attn_cache_kernel(
+    attn_args a) {
     constexpr int NT = terms_of<T>, TR = XT * TILE;
     __shared__ float so[WAVES][TR][D + 4];
     __shared__ float sml[WAVES][TR][2];
@@ -634,7 +643,7 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (hit[i] != 0.f) st.o[c][i] = __uint_as_float(0x7fc00000u);
+            st.o[c][i] += nan_if(hit[i]);
     }
 }
 

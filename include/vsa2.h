@@ -612,7 +612,12 @@ vsa2_status vsa2_cache_read(const vsa2_cache* c, int32_t dtype, int32_t n, const
  *                                               the last count[b] of the list)
  *   limit = 0 for i >= count[b].
  *   dtype   of q and o; products are exact in the cached codes, and fp32
- *           queries and probabilities enter them as three bf16 terms.
+ *           queries and probabilities enter them as three bf16 terms.  With bf16
+ *           queries probabilities are fp16 there: 11 bits of each, an eighth of
+ *           the result's rounding; of those (times the value row's power) below
+ *           2^-21 of a row's largest 2^-32 of that, or 2^-13 and 2^-24 where that
+ *           one's value row is far smaller than others of the list.  Value rows
+ *           below 2^-126 of the list's largest count as zeros.
  *   q, o    rows (batch, heads_q, n); o is written.
  *   lse     [batch][heads_q][n] fp32 natural-log log-sum-exp.
  *   length  device int32 [batch] (clamped to [0, 64 max_pages]); count device

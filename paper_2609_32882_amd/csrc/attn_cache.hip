@@ -2,14 +2,20 @@
 //
 // Rows: the query heads of one KV head times the call's tokens (token-major), in
 // tiles of 16 (or pairs of them, or 128).  Everything is computed transposed, S^T = K Q^T and
-// O^T = V^T P^T on 16x16x32 bf16 MFMAs, so that a lane holds one row (column
+// O^T = V^T P^T on 16x16x32 MFMAs, so that a lane holds one row (column
 // lane % 16) through the whole kernel: the softmax needs two exchanges a page,
 // P goes from the accumulators of the first product into the operand of the
 // second without leaving its lane (the page's V order is made for that), and O
-// is rescaled lane by lane.  e4m3 codes become bf16 exactly: K's with the
-// token's power applied by the conversion, V's plain, with the power on P.
-// fp32 queries and probabilities are three bf16 terms each, so their products
-// lose nothing that fp32 sums would keep.
+// is rescaled lane by lane.  e4m3 codes become 16-bit values exactly: K's bf16,
+// with the token's power applied by the conversion, V's plain, with the power
+// on P.  fp32 queries and probabilities are three bf16 terms each, so their
+// products lose nothing that fp32 sums would keep.  For bf16 queries P and V
+// are fp16: 11 bits of a weight, where bf16's 8 would cost as much as the
+// result's own rounding.  fp16's exponents do not reach far: P is scaled by a
+// power of two that makes the largest power seen 2^7, and in rows whose weight is
+// on tokens of much smaller powers by one more (row_softmax).  Measured against
+// bf16 P: 2.5% of the time at 1,792 rows, 3 to 9% over a few rows where codes and
+// weights bound a page (D = 64), none where memory does.
 //
 // Bound by memory for single tokens: 2 (D + 1) bytes per token and KV head.  A
 // page is 16 KB in runs of 1 KB per load instruction; the waves of a workgroup
@@ -49,9 +55,17 @@ struct attn_args {
 
 template <typename T> constexpr int terms_of = sizeof(T) == 4 ? 3 : 1;
 
-// 8 values as the sum of bf16 fragments: three for fp32 (24 bits); one for bf16, where
-// queries are exact and probabilities rounded to 8 bits, an error below the rounding of
-// the inputs themselves (the sum of the weights keeps 32).
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8_t;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_vt;
+struct frag_f16 { f16x8_t v; };
+
+// P and V: fp16 for bf16 queries, three bf16 terms and bf16 for fp32.
+template <typename T> struct weight_frag { using type = frag_f16; };
+template <> struct weight_frag<float> { using type = frag_bf16; };
+template <typename T> using weight_frag_t = typename weight_frag<T>::type;
+
+// 8 values as the sum of bf16 fragments: three for fp32 (24 bits), one for bf16 queries
+// (exact).
 template <int N>
 __device__ __forceinline__ void split_frag(frag_bf16* f, const float* x) {
     if constexpr (N == 1) {
@@ -64,6 +78,35 @@ __device__ __forceinline__ void split_frag(frag_bf16* f, const float* x) {
         for (int i = 0; i < 8; ++i) rest[i] = x[i] - static_cast<float>(f[0].v[i]);
         pack_frag_hilo(f[1], f[2], rest);
     }
+}
+
+// 8 probabilities times their powers: three bf16 terms, or fp16, whose rounding (2^-12 of a
+// weight at most, against the result's 2^-9) is the one to fewer bits before the result.
+template <int N>
+__device__ __forceinline__ void split_weights(frag_bf16* f, const float* x) { split_frag<N>(f, x); }
+template <int N>
+__device__ __forceinline__ void split_weights(frag_f16* f, const float* x) {
+    static_assert(N == 1, "one term");
+    typedef __attribute__((ext_vector_type(2))) float f32x2_vt;
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+    u32x4_t w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2_vt y = {x[2 * i], x[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, f16x2_vt));
+    }
+    f[0].v = __builtin_bit_cast(f16x8_t, w);
+}
+
+// 8 e4m3 codes in fp16 or bf16 (exact).
+__device__ __forceinline__ void decode_values(frag_f16& f, uint32_t a, uint32_t b) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+    u32x4_t w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(a), 1.f, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(a), 1.f, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(b), 1.f, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(b), 1.f, true));
+    f.v = __builtin_bit_cast(f16x8_t, w);
 }
 
 // 8 e4m3 codes times a power of two, in bf16 (exact).
@@ -79,8 +122,16 @@ __device__ __forceinline__ frag_bf16 decode8(uint32_t a, uint32_t b, float power
     return f;
 }
 
+__device__ __forceinline__ void decode_values(frag_bf16& f, uint32_t a, uint32_t b) { f = decode8(a, b, 1.f); }
+
 __device__ __forceinline__ f32x4_t mma16(const frag_bf16& a, const frag_bf16& b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mma16(const frag_f16& a, const frag_f16& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x16_t& c, const frag_f16& a, const frag_f16& b) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, b.v, c, 0, 0, 0);
 }
 
 __device__ __forceinline__ float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -146,6 +197,85 @@ __device__ __forceinline__ float groups_max(float x) {
     return halves_max(fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])));
 }
 
+// A row's running maximum and sum (base 2).  Weights are 2^(score - m), m = base + lift.
+//
+// fp16 weights: P = weight times 2^(power - E + 7 + lift).  E is the largest power the wave has
+// seen, so that without a lift no P passes 2^15 (weights are at most 2^8).  A row whose weight lies
+// on tokens of far smaller powers has P far below: its lift raises those.  `top` is log2 of weight
+// times 2^(power - E) at its largest when that was last looked at, or up to 7 less (a look takes the
+// powers of a page to be 2^7 below E unless one of them is less), and a lift takes it to 0 from below
+// -8.  So the largest P is 2^-1 at least, 2^7 where powers are alike: fp16 keeps 11 bits of every P
+// down to 2^-13 (2^-21) of a row's largest, and the error of the others is 2^-24 (2^-32) of that at
+// most.
+template <bool LIFTED>
+struct row_softmax {
+    static constexpr float NONE = -FLT_MAX;      // base of a row that has seen nothing
+    float base = NONE, l = 0.f, top = 0.f, down = 1.f;     // down: 2^-lift
+    __device__ __forceinline__ float lift() const {
+        return LIFTED ? static_cast<float>(127 - static_cast<int>(__float_as_uint(down) >> 23)) : 0.f;
+    }
+    __device__ __forceinline__ float m() const { return base == NONE ? -INFINITY : base + lift(); }
+    // The maximum goes to `up`, 2^-E changes by 2^de, some weights times 2^(power - E) are then
+    // 2^most: what O is multiplied with.  One factor, since the scales alone may leave fp32.
+    __device__ __forceinline__ float move(float up, float de, float most) {
+        const float was = lift(), by = base == NONE ? NONE : base + was - up;
+        l *= fast_exp2(by);
+        if constexpr (!LIFTED) {
+            base = up;
+            return fast_exp2(by);
+        }
+        top = fmaxf(top + by + de, most);
+        const float now = top < -8.f ? fminf(-floorf(top), 110.f) : 0.f;
+        base = up == NONE ? NONE : up - now;
+        down = power_of(static_cast<uint32_t>(127 - static_cast<int>(now)));
+        return fast_exp2(by + de + (now - was));
+    }
+};
+template <typename T> constexpr bool lifted_of = sizeof(T) == 2;
+template <typename T> using row_softmax_t = row_softmax<lifted_of<T>>;
+
+// The exponents (+ 127) of a wave's powers, the same in every lane: the largest so far (E), what it
+// was before the page at hand, and whether some token of the page lies more than 2^7 below.
+struct powers_seen {
+    int most = 0, was = 0;
+    bool wide = false;
+    // Is one of the marked bytes of four powers above E, or more than 2^7 below?
+    __device__ __forceinline__ bool news(uint32_t four, uint32_t marked) const {
+        return ((four - static_cast<uint32_t>(most - 7) * 0x01010101u) & 0xf8f8f8f8u & marked) != 0;
+    }
+    // `marked`: those of the page's (or pages') in every lane, all of them together; the others 0.
+    __device__ __forceinline__ void look(uint32_t marked) {
+        const uint32_t ev = max(marked & 0xffu, (marked >> 8) & 0xffu), od = max((marked >> 16) & 0xffu, marked >> 24);
+        float x = static_cast<float>(max(ev, od));
+        x = fmaxf(x, dpp_f32<0xB1>(x));
+        x = fmaxf(x, dpp_f32<0x4E>(x));
+        x = fmaxf(x, dpp_f32<0x141>(x));
+        x = fmaxf(x, dpp_f32<0x140>(x));
+        was = most;
+        most = max(most, __builtin_amdgcn_readfirstlane(static_cast<int>(groups_max(x))));
+        bool less = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int byte = static_cast<int>((marked >> (8 * i)) & 0xffu);
+            less |= byte != 0 && byte < most - 7;
+        }
+        wide = __ballot(less) != 0;
+    }
+    // 2^(power - E + 7), of a byte that raised() gave where the powers are wide
+    __device__ __forceinline__ float scaled(uint32_t byte) const {
+        return __uint_as_float((byte << 23) + (static_cast<uint32_t>(134 - most) << 23));
+    }
+    // At least what scaled() gives 0 for.
+    __device__ __forceinline__ uint32_t raised(uint32_t byte) const {
+        return static_cast<uint32_t>(max(static_cast<int>(byte), most - 134));
+    }
+    // what takes O back
+    __device__ __forceinline__ float back(const row_softmax<true>& w) const {
+        return most == 0 ? 0.f : ldexpf(w.down, most - 134);
+    }
+    __device__ __forceinline__ float back(const row_softmax<false>&) const { return 1.f; }
+};
+
 // Valid pages of a list's piece [lo, hi) in order: 64 table entries at a time in
 // a register, a bit for each that names a page.
 struct page_walk {
@@ -206,9 +336,9 @@ __device__ __forceinline__ const int32_t* list_of(const attn_args& a, int b, int
 
 // One row tile's state in one wave: its running maximum and sum (base 2) and
 // O^T, rows d = 16 c + 4 g + i, column lane % 16.
-template <int D>
+template <typename T, int D>
 struct tile_state {
-    float m, l;
+    row_softmax_t<T> w;
     f32x4_t o[D / 16];
 };
 
@@ -229,6 +359,8 @@ __device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
     pd.ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + (lane >> 4) * 16);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) pd.v[i] = vp[i * 64];
+    // all of them requested before the first is waited for
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // One page for XT tiles, decoded once for all of them.  MASKED: some row's limit,
@@ -236,7 +368,7 @@ __device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
 template <typename T, int D, int XT, bool MASKED>
 __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos, const int (&limit)[XT], int lim_max,
                                           const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], float scale,
-                                          tile_state<D> (&st)[XT]) {
+                                          tile_state<T, D> (&st)[XT], powers_seen& seen) {
     constexpr int NT = terms_of<T>;
     const int g = lane_id() >> 4;
     f32x4_t s[XT][4];
@@ -258,11 +390,18 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
                 }
         }
     }
-    const uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
+    uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
     uint4 vr[D / 16];
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) vr[c] = pd.v[c];
-    frag_bf16 pf[XT][2][NT];
+    weight_frag_t<T> pf[XT][2][NT];
+    // a quarter of the lane's tokens' powers, of those below lim_max
+    const int at = lane_id() & 3;
+    const uint32_t four = at & 2 ? (at & 1 ? vw[3] : vw[2]) : (at & 1 ? vw[1] : vw[0]);
+    uint32_t marked = ~0u;
+    if constexpr (MASKED) marked = first_bytes(lim_max - (pos + 16 * at + 4 * g));
+    float mx[XT];
+    bool far = NT == 1 && seen.news(four, marked);
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         if constexpr (MASKED) {
@@ -272,38 +411,69 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
                 for (int i = 0; i < 4; ++i)
                     if (pos + 16 * t + 4 * g + i >= limit[x]) s[x][t][i] = -INFINITY;
         }
-        float mx = -INFINITY;
+        mx[x] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) mx = fmaxf(fmaxf(mx, s[x][t][i]), s[x][t][i + 1]);
-        mx = groups_max(mx) * scale;
-        // the running maximum moves only when it would grow by more than 8
-        // (weights up to 2^8 of the first): most pages leave O alone
-        if (__ballot(mx > st[x].m + 8.f) != 0) {
-            const float up = fmaxf(st[x].m, mx);
-            const float f = up == -INFINITY ? 1.f : fast_exp2(st[x].m - up);
-            st[x].m = up;
-            st[x].l *= f;
+            for (int i = 0; i < 4; i += 2) mx[x] = fmaxf(fmaxf(mx[x], s[x][t][i]), s[x][t][i + 1]);
+        mx[x] = groups_max(mx[x]);
+        far |= fmaf(mx[x], scale, -st[x].w.base) > 8.f;
+    }
+    // the running maxima move only when one would grow by more than 8 (weights
+    // up to 2^8 of the first), less with a lift: most pages leave O alone
+    if (__ballot(far) != 0) {
+        if constexpr (NT == 1) {
+            seen.look(four & marked);
+            if (seen.wide) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    uint32_t w = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w |= seen.raised((vw[t] >> (8 * i)) & 0xffu) << (8 * i);
+                    vw[t] = w;
+                }
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < XT; ++x) {
+            row_softmax_t<T>& w = st[x].w;
+            const float up = fmaxf(w.base + w.lift(), mx[x] * scale);
+            float most = fmaf(mx[x], scale, -up) - 7.f;
+            if (NT == 1 && seen.wide) {
+                most = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        most = fmaxf(most, fmaf(s[x][t][i], scale, -up) +
+                                               static_cast<float>(static_cast<int>((vw[t] >> (8 * i)) & 0xffu) - seen.most));
+                most = groups_max(most);
+            }
+            const float f = w.move(up, static_cast<float>(seen.was - seen.most), most);
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) st[x].o[c] *= f;
         }
-        const float base = st[x].m == -INFINITY ? 0.f : st[x].m;
-        float p[4][4];
+    }
+#pragma unroll
+    for (int x = 0; x < XT; ++x) {
+        row_softmax_t<T>& w = st[x].w;
+        float p[4][4], sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = fast_exp2(fmaf(s[x][t][i], scale, -base));
-                st[x].l += e;
+                const float e = fast_exp2(fmaf(s[x][t][i], scale, -w.base));
+                sum += e;
                 // a masked place's power may be anything
-                p[t][i] = MASKED && e == 0.f ? 0.f : e * power_of((vw[t] >> (8 * i)) & 0xffu);
+                const uint32_t byte = (vw[t] >> (8 * i)) & 0xffu;
+                p[t][i] = MASKED && e == 0.f ? 0.f : e * (NT == 1 ? seen.scaled(byte) : power_of(byte));
             }
+        w.l = fmaf(sum, w.down, w.l);
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             const float z[8] = {p[2 * y][0], p[2 * y][1], p[2 * y][2], p[2 * y][3],
                                 p[2 * y + 1][0], p[2 * y + 1][1], p[2 * y + 1][2], p[2 * y + 1][3]};
-            split_frag<NT>(pf[x][y], z);
+            split_weights<NT>(pf[x][y], z);
         }
     }
     uint32_t keep[4], any = 0;
@@ -327,7 +497,9 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
     }
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
-        const frag_bf16 v0 = decode8(vr[c].x, vr[c].y, 1.f), v1 = decode8(vr[c].z, vr[c].w, 1.f);
+        weight_frag_t<T> v0, v1;
+        decode_values(v0, vr[c].x, vr[c].y);
+        decode_values(v1, vr[c].z, vr[c].w);
 #pragma unroll
         for (int y = NT - 1; y >= 0; --y)
 #pragma unroll
@@ -414,7 +586,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
     else if (lo < hi) walk.fetch(mine);
 
     frag_bf16 qf[XT][D / 32][NT];
-    tile_state<D> st[XT];
+    tile_state<T, D> st[XT];
+    powers_seen seen;
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         const int r = tile * TR + x * TILE + col;
@@ -429,8 +602,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
             }
             split_frag<NT>(qf[x][u], y);
         }
-        st[x].m = -INFINITY;
-        st[x].l = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) st[x].o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
@@ -442,25 +613,27 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2, D
     for (; whole(); more = walk.next(pg, id, mine)) {
         page_data<D> x;
         load_page<D>(x, page());
-        page_step<T, D, XT, false>(x, nullptr, 0, limit, lim_max, qf, scale, st);
+        page_step<T, D, XT, false>(x, nullptr, 0, limit, lim_max, qf, scale, st, seen);
     }
     for (; more; more = walk.next(pg, id, mine)) {
         page_data<D> x;
         load_page<D>(x, page());
-        page_step<T, D, XT, true>(x, page(), pg * CACHE_TOKENS, limit, lim_max, qf, scale, st);
+        page_step<T, D, XT, true>(x, page(), pg * CACHE_TOKENS, limit, lim_max, qf, scale, st, seen);
     }
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
-        float l = st[x].l;
+        float l = st[x].w.l;
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
         const bool dead = limit[x] == 0;
         const int row = x * TILE + col;
+        const float back = seen.back(st[x].w);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c)
-            *reinterpret_cast<f32x4_t*>(&so[wave][row][16 * c + 4 * g]) = dead ? f32x4_t{0.f, 0.f, 0.f, 0.f} : st[x].o[c];
+            *reinterpret_cast<f32x4_t*>(&so[wave][row][16 * c + 4 * g]) =
+                dead ? f32x4_t{0.f, 0.f, 0.f, 0.f} : st[x].o[c] * back;
         if (g == 0) {
-            sml[wave][row][0] = dead ? -INFINITY : st[x].m;
+            sml[wave][row][0] = dead ? -INFINITY : st[x].w.m();
             sml[wave][row][1] = dead ? 0.f : l;
         }
     }
@@ -525,18 +698,50 @@ __device__ __forceinline__ void copy_page(char* lds, const char* page, int wave,
 
 // A wave's 32 rows: running maximum and sum (base 2), O^T of column lane % 32,
 // elements 32 c + 8 (i / 4) + 4 (lane / 32) + i % 4.
-template <int D>
+template <typename T, int D>
 struct rows_state {
-    float m, l;
+    row_softmax_t<T> w;
     f32x16_t o[D / 32];
 };
+
+// Moves the running maximum, and the scale of P, for the scores s of N / 2 pages, whose powers
+// are power[page][1]; `mx` is their largest.  Most pages leave O alone: see page_step.
+template <typename T, int D, int N>
+__device__ __forceinline__ void rows_move(const f32x16_t (&s)[N], const float (*power)[2][64], float mx, float scale,
+                                          powers_seen& seen, rows_state<T, D>& st) {
+    constexpr bool LIFTED = lifted_of<T>;
+    bool far = fmaf(mx, scale, -st.w.base) > 8.f;
+    if constexpr (LIFTED) far |= seen.was != seen.most;
+    if (__ballot(far) == 0) return;
+    const float up = fmaxf(st.w.base + st.w.lift(), mx * scale);
+    float most = fmaf(mx, scale, -up) - 7.f;
+    if (LIFTED && seen.wide) {
+        const int h2 = lane_id() >> 5;
+        most = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float pw = power[t / 2][1][(t % 2) * 32 + 8 * (i / 4) + 4 * h2 + i % 4];
+                most = fmaxf(most, fmaf(s[t][i], scale, -up) + static_cast<float>(static_cast<int>(__float_as_uint(pw) >> 23) - 134));
+            }
+        most = halves_max(most);
+    }
+    const float f = st.w.move(up, static_cast<float>(seen.was - seen.most), most);
+    seen.was = seen.most;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
+}
 
 // One page in LDS for a wave's rows, where some row's limit, or the list's end,
 // may lie inside it.
 template <typename T, int D>
-__device__ __forceinline__ void rows_step(const char* kp, const char* vp, const float (*power)[64], int first, int limit,
-                                          int wmax, const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale,
-                                          rows_state<D>& st) {
+__device__ __forceinline__ void rows_step(const char* kp, const char* vp, const float (*page_power)[2][64], int first,
+                                          int limit, int wmax, const frag_bf16 (&qf)[D / 32][2][terms_of<T>],
+                                          float scale, powers_seen& seen, rows_state<T, D>& st) {
+    const float (*power)[64] = *page_power;
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
     const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
     f32x16_t s[2];
@@ -566,28 +771,17 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
-    mx = halves_max(mx) * scale;
-    // the running maximum moves only when it would grow by more than 8
-    // (weights up to 2^8 of the first): most pages leave O alone
-    if (__ballot(mx > st.m + 8.f) != 0) {
-        const float up = fmaxf(st.m, mx);
-        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
-        st.m = up;
-        st.l *= f;
-#pragma unroll
-        for (int c = 0; c < VC; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
-    }
-    const float base = st.m == -INFINITY ? 0.f : st.m;
-    frag_bf16 pf[4][NT];
+    mx = halves_max(mx);
+    rows_move<T, D>(s, page_power, mx, scale, seen, st);
+    float sum = 0.f;
+    weight_frag_t<T> pf[4][NT];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            y[i] = fast_exp2(fmaf(s[t / 2][(t % 2) * 8 + i], scale, -base));
-            st.l += y[i];
+            y[i] = fast_exp2(fmaf(s[t / 2][(t % 2) * 8 + i], scale, -st.w.base));
+            sum += y[i];
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -599,8 +793,9 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
                 y[4 * x + i] = y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
             }
         }
-        split_frag<NT>(pf[t], y);
+        split_weights<NT>(pf[t], y);
     }
+    st.w.l = fmaf(sum, st.w.down, st.w.l);
     uint32_t keep[4][2], any = 0;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -621,7 +816,8 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
                 w[t][x] &= ~nan;
                 any |= nan;
             }
-            const frag_bf16 vf = decode8(w[t][0], w[t][1], 1.f);
+            weight_frag_t<T> vf;
+            decode_values(vf, w[t][0], w[t][1]);
 #pragma unroll
             for (int z = NT - 1; z >= 0; --z) mma(st.o[c], vf, pf[t][z]);
         }
@@ -650,7 +846,8 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
 // The two pages of a stage together, no limit inside either.
 template <typename T, int D>
 __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase, const float (*power)[2][64],
-                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale, rows_state<D>& st) {
+                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale, powers_seen& seen,
+                                          rows_state<T, D>& st) {
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
     const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
     f32x16_t s[4];
@@ -676,29 +873,19 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[t][i]), s[t][i + 1]);
-    mx = halves_max(mx) * scale;
-    if (__ballot(mx > st.m + 8.f) != 0) {
-        const float up = fmaxf(st.m, mx);
-        const float f = up == -INFINITY ? 1.f : fast_exp2(st.m - up);
-        st.m = up;
-        st.l *= f;
-#pragma unroll
-        for (int c = 0; c < VC; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
-    }
-    const float base = st.m == -INFINITY ? 0.f : st.m;
+    mx = halves_max(mx);
+    rows_move<T, D>(s, power, mx, scale, seen, st);
     float l2[2] = {0.f, 0.f};
 #pragma unroll
     for (int pg = 0; pg < 2; ++pg) {
         const char* vp = lds + pg * 128 * D + vbase;
-        frag_bf16 pf[4][NT];
+        weight_frag_t<T> pf[4][NT];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             float y[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                y[i] = fast_exp2(fmaf(s[2 * pg + t / 2][(t % 2) * 8 + i], scale, -base));
+                y[i] = fast_exp2(fmaf(s[2 * pg + t / 2][(t % 2) * 8 + i], scale, -st.w.base));
                 l2[i & 1] += y[i];
             }
 #pragma unroll
@@ -708,7 +895,7 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) y[4 * x + i] *= pv[i];
             }
-            split_frag<NT>(pf[t], y);
+            split_weights<NT>(pf[t], y);
         }
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
@@ -717,13 +904,14 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
             const uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const frag_bf16 vf = decode8(w[t][0], w[t][1], 1.f);
+                weight_frag_t<T> vf;
+            decode_values(vf, w[t][0], w[t][1]);
 #pragma unroll
                 for (int z = NT - 1; z >= 0; --z) mma(st.o[c], vf, pf[t][z]);
             }
         }
     }
-    st.l += l2[0] + l2[1];
+    st.w.l = fmaf(l2[0] + l2[1], st.w.down, st.w.l);
 }
 
 template <typename T, int D>
@@ -781,9 +969,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
             }
             split_frag<NT>(qf[w][z], y);
         }
-    rows_state<D> st;
-    st.m = -INFINITY;
-    st.l = 0.f;
+    rows_state<T, D> st;
+    powers_seen seen;
 #pragma unroll
     for (int c = 0; c < VC; ++c)
 #pragma unroll
@@ -817,10 +1004,22 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     // hand.  Past the barrier every wave is done with the other buffer.
     int at[STAGE];
     auto turn = [&]() {
+        if constexpr (NT == 1) {
+            uint32_t powers = 0, marked = 0;
+#pragma unroll
+            for (int x = 0; x < STAGE; ++x) {
+                const uint32_t here = x < have && pos[x] * CACHE_TOKENS + lane < wmax ? 0xffu << (8 * x) : 0u;
+                powers |= static_cast<uint32_t>(ve[x]) << (8 * x);
+                marked |= here;
+            }
+            seen.was = seen.most;
+            seen.wide = false;
+            if (__ballot(seen.news(powers, marked)) != 0) seen.look(powers & marked);
+        }
 #pragma unroll
         for (int x = 0; x < STAGE; ++x) {
             power[wave][x][0][lane] = power_of(ke[x]);
-            power[wave][x][1][lane] = power_of(ve[x]);
+            power[wave][x][1][lane] = NT == 1 ? seen.scaled(seen.raised(ve[x])) : power_of(ve[x]);
             at[x] = pos[x];
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -831,7 +1030,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     };
     while (have == STAGE && pos[STAGE - 1] < full) {
         turn();
-        rows_pair<T, D>(codes[buf][0], kbase, vbase, power[wave], qf, scale, st);
+        rows_pair<T, D>(codes[buf][0], kbase, vbase, power[wave], qf, scale, seen, st);
         buf ^= 1;
     }
     while (have > 0) {
@@ -840,13 +1039,18 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
         for (int x = 0; x < n; ++x) {
             const int first = (x ? at[STAGE - 1] : at[0]) * CACHE_TOKENS;
             if (first < wmax)
-                rows_step<T, D>(codes[buf][x] + kbase, codes[buf][x] + vbase, power[wave][x], first, limit, wmax, qf,
-                                      scale, st);
+                rows_step<T, D>(codes[buf][x] + kbase, codes[buf][x] + vbase, &power[wave][x], first, limit, wmax, qf,
+                                      scale, seen, st);
         }
         buf ^= 1;
     }
     f32x16_t(&o)[VC] = st.o;
-    float m = st.m, l = st.l;
+    float m = st.w.m(), l = st.w.l;
+    const float back = seen.back(st.w);
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= back;
     l += swap_half(l);
     if (limit == 0) {
         m = -INFINITY;

@@ -634,22 +634,22 @@ class Rope:
     [batch, 3] position of each sequence's first token (None: the grid's own),
     and which elements pair up ("adjacent" or "halves")."""
 
-    __slots__ = ("c", "tables", "origin")
+    __slots__ = ("c", "tables", "origin", "device")
     PAIRINGS = {"adjacent": VSA2_ROPE_ADJACENT, "halves": VSA2_ROPE_HALVES}
 
     def __init__(self, axes, tables, origin=None, pairing="adjacent"):
         self.c = vsa2_rope()
         pairs = self.PAIRINGS[pairing]
-        _marshal().fill_rope(self.c, axes, tables, origin, pairs)
+        self.device = _marshal().fill_rope(self.c, axes, tables, origin, pairs)
         self.tables, self.origin = tuple(tables), origin       # kept alive with their addresses
 
 
 def _rope_c(rope, p):
     if rope is None:
-        return None
+        return None, -1
     if rope.origin is not None and rope.origin.shape[0] != p.batch:
         raise ValueError("origin: expected %d sequences, got %d" % (p.batch, rope.origin.shape[0]))
-    return rope.c
+    return rope.c, rope.device
 
 
 def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None, eps=0.0, out=None):
@@ -659,7 +659,8 @@ def qk_norm_rope(p, q=None, k=None, v=None, q_gain=None, k_gain=None, rope=None,
     (views of a fused projection are fine); each may be None.  Returns (q, k, v)
     contiguous; `out` gives the three outputs."""
     p = problem_from(p)
-    return _marshal().norm_rope(p, _rope_c(rope, p), eps, q, k, v, q_gain, k_gain, out, _stream)
+    r, device = _rope_c(rope, p)
+    return _marshal().norm_rope(p, r, eps, q, k, v, q_gain, k_gain, out, _stream, device)
 
 
 def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, k_gain=None, rope=None, eps=0.0,
@@ -670,7 +671,8 @@ def qk_norm_rope_bwd(p, dq=None, dk=None, dv=None, q=None, k=None, q_gain=None, 
     fused gradient are fine).  q and k are the forward's inputs, needed with the
     norm; the gains' gradients come with them."""
     p = problem_from(p)
-    return _marshal().norm_rope_bwd(p, _rope_c(rope, p), eps, dq, dk, dv, q, k, q_gain, k_gain, out, _stream)
+    r, device = _rope_c(rope, p)
+    return _marshal().norm_rope_bwd(p, r, eps, dq, dk, dv, q, k, q_gain, k_gain, out, _stream, device)
 
 
 class KVCache:
@@ -678,11 +680,11 @@ class KVCache:
     and `table` int32 [batch, max_pages], or [batch, heads_kv, max_pages] with a
     list of pages for every KV head (include/vsa2.h has the page's layout)."""
 
-    __slots__ = ("c", "pool", "table")
+    __slots__ = ("c", "pool", "table", "device")
 
     def __init__(self, pool, table):
         self.c = vsa2_cache()
-        _marshal().fill_cache(self.c, pool, table)
+        self.device = _marshal().fill_cache(self.c, pool, table)
         self.pool, self.table = pool, table             # kept alive with their addresses
 
     @classmethod
@@ -697,7 +699,7 @@ def cache_write(cache, k, v, start, count=None):
     """Quantise tokens k, v [batch, heads_kv, n, D] (any strides) into the cache:
     token i < count[b] (int32 [batch], None: all n) goes to list position
     start[b] + i (int32 [batch])."""
-    _marshal().cache_write(cache.c, k, v, start, count, _stream)
+    _marshal().cache_write(cache.c, k, v, start, count, _stream, cache.device)
 
 
 def cache_read(cache, n, start, count=None, dtype=None, out=None):
@@ -706,7 +708,7 @@ def cache_read(cache, n, start, count=None, dtype=None, out=None):
     says float32.  `out` gives the two outputs (any strides)."""
     dt = VSA2_BF16 if dtype is None else _vdtype(dtype)
     k, v = (None, None) if out is None else out
-    return _marshal().cache_read(cache.c, cache.pool, n, start, count, dt, k, v, _stream)
+    return _marshal().cache_read(cache.c, cache.pool, n, start, count, dt, k, v, _stream, cache.device)
 
 
 def attn_cache(cache, q, length, count=None, causal=False, o=None):
@@ -714,4 +716,4 @@ def attn_cache(cache, q, length, count=None, causal=False, o=None):
     first length[b] list positions; causal: the call's tokens are the last
     count[b] (None: n) of them and see no later one.  Returns (o, lse), o like q
     and contiguous unless given, lse [batch, heads_q, n] fp32."""
-    return _marshal().attn_cache(cache.c, q, length, count, True if causal else False, o, _stream)
+    return _marshal().attn_cache(cache.c, q, length, count, True if causal else False, o, _stream, cache.device)

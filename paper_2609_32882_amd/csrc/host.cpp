@@ -51,6 +51,15 @@ void on_current_device(const at::Tensor& t, const char* name) {
         fail(std::string(name) + ": on " + t.device().str() + ", but the current device is cuda:" + std::to_string(t_device));
 }
 
+// Nor the memory whose addresses a structure has kept: `device` is the one it was filled on (-1: none).
+int32_t integer32(PyObject* o, const char* name);
+void filled_here(PyObject* device, const char* name) {
+    const int32_t d = integer32(device, name);
+    if (d >= 0 && d != t_device)
+        fail(std::string(name) + ": its tensors are on cuda:" + std::to_string(d) + ", but the current device is cuda:" +
+             std::to_string(t_device));
+}
+
 // The tensor in a Python object; null for None.
 const at::Tensor* tensor(PyObject* o, const char* name) {
     if (o == Py_None) return nullptr;
@@ -164,7 +173,7 @@ void count_args(Py_ssize_t n, Py_ssize_t want) {
     }
 }
 
-// (structure, axes, tables, origin, pairing)
+// (structure, axes, tables, origin, pairing) -> the device of the tables and origin, -1 without any
 PyObject* fill_rope(PyObject* const* a, Py_ssize_t n) {
     count_args(n, 5);
     vsa2_rope* r = structure<vsa2_rope>(a[0], "rope");
@@ -185,10 +194,10 @@ PyObject* fill_rope(PyObject* const* a, Py_ssize_t n) {
     const at::Tensor* origin = tensor(a[3], "origin");
     r->origin = origin ? contiguous<int32_t>(origin, {origin->dim() ? origin->size(0) : 0, 3}, at::kInt, "origin") : nullptr;
     r->pairing = integer32(a[4], "pairing");
-    Py_RETURN_NONE;
+    return PyLong_FromLong(r->axis[0] || r->axis[1] || r->axis[2] || origin ? t_device : -1);
 }
 
-// (structure, pool, table)
+// (structure, pool, table) -> their device
 PyObject* fill_cache(PyObject* const* a, Py_ssize_t n) {
     count_args(n, 3);
     vsa2_cache* c = structure<vsa2_cache>(a[0], "cache");
@@ -209,14 +218,15 @@ PyObject* fill_cache(PyObject* const* a, Py_ssize_t n) {
     c->pages = static_cast<int32_t>(pool.size(0));
     c->max_pages = static_cast<int32_t>(table.size(-1));
     c->table_heads = lists ? c->heads_kv : 1;
-    Py_RETURN_NONE;
+    return PyLong_FromLong(t_device);
 }
 
 const vsa2_rope* rope_or_null(PyObject* o) { return o == Py_None ? nullptr : structure<vsa2_rope>(o, "rope"); }
 
-// (problem, rope, eps, q, k, v, q_gain, k_gain, out, stream) -> (q, k, v)
+// (problem, rope, eps, q, k, v, q_gain, k_gain, out, stream, rope's device) -> (q, k, v)
 PyObject* norm_rope(PyObject* const* a, Py_ssize_t n) {
-    count_args(n, 10);
+    count_args(n, 11);
+    filled_here(a[10], "rope");
     const vsa2_problem& p = *structure<vsa2_problem>(a[0], "problem");
     const vsa2_rope* r = rope_or_null(a[1]);
     const at::ScalarType dt = dtype_of(p);
@@ -251,10 +261,11 @@ PyObject* norm_rope(PyObject* const* a, Py_ssize_t n) {
     return t;
 }
 
-// (problem, rope, eps, dq, dk, dv, q, k, q_gain, k_gain, out, stream)
+// (problem, rope, eps, dq, dk, dv, q, k, q_gain, k_gain, out, stream, rope's device)
 //   -> (dq_in, dk_in, dv_in, dq_gain, dk_gain)
 PyObject* norm_rope_bwd(PyObject* const* a, Py_ssize_t n) {
-    count_args(n, 12);
+    count_args(n, 13);
+    filled_here(a[12], "rope");
     const vsa2_problem& p = *structure<vsa2_problem>(a[0], "problem");
     const vsa2_rope* r = rope_or_null(a[1]);
     const float eps = static_cast<float>(real(a[2]));
@@ -313,9 +324,10 @@ PyObject* norm_rope_bwd(PyObject* const* a, Py_ssize_t n) {
     return t;
 }
 
-// (cache, k, v, start, count, stream)
+// (cache, k, v, start, count, stream, cache's device)
 PyObject* cache_write(PyObject* const* a, Py_ssize_t n) {
-    count_args(n, 6);
+    count_args(n, 7);
+    filled_here(a[6], "cache");
     const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
     const at::Tensor &k = required(a[1], "k"), &v = required(a[2], "v");
     const at::ScalarType dt = k.scalar_type();
@@ -330,9 +342,10 @@ PyObject* cache_write(PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// (cache, pool, n, start, count, dtype, k, v, stream) -> (k, v); dtype is the code of new outputs
+// (cache, pool, n, start, count, dtype, k, v, stream, cache's device) -> (k, v); dtype is the code of new outputs
 PyObject* cache_read(PyObject* const* a, Py_ssize_t n) {
-    count_args(n, 9);
+    count_args(n, 10);
+    filled_here(a[9], "cache");
     const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
     const int32_t tokens = integer32(a[2], "n");
     if (tokens < 0) fail("n: expected 0 or more");
@@ -363,9 +376,10 @@ PyObject* cache_read(PyObject* const* a, Py_ssize_t n) {
     return t;
 }
 
-// (cache, q, length, count, causal, o, stream) -> (o, lse)
+// (cache, q, length, count, causal, o, stream, cache's device) -> (o, lse)
 PyObject* attn_cache(PyObject* const* a, Py_ssize_t n) {
-    count_args(n, 7);
+    count_args(n, 8);
+    filled_here(a[7], "cache");
     const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
     const at::Tensor& q = required(a[1], "q");
     if (q.dim() != 4 || q.size(1) > INT32_MAX || q.size(2) > INT32_MAX)

@@ -115,3 +115,16 @@ def test_small_values_under_the_weight_beside_large_ones_without():
             q = torch.full((1, 1, n, D), 8.0).bfloat16().cuda()       # logits of 512 and -512
             o, _ = vsa2.attn_cache(cache, q, torch.tensor([200], dtype=torch.int32).cuda())
             assert (o == 2.0 ** -30).all()
+
+
+@pytest.mark.parametrize("n", [1, 20, 140])
+def test_large_values_without_weight_after_small_ones_with_it(n):
+    """The weight is on the first page, whose values are 2^-70 of the later pages'."""
+    D, m = 64, 500
+    k, v = torch.full((1, 2, m, D), -8.0), torch.full((1, 2, m, D), 2.0 ** 30)
+    k[:, :, 3], v[:, :, :64] = 8.0, 2.0 ** -40
+    cache = vsa2.KVCache.empty(torch.arange(8, dtype=torch.int32).view(1, 8).cuda(), 8, 2, D)
+    vsa2.cache_write(cache, k.cuda(), v.cuda(), torch.zeros(1, dtype=torch.int32).cuda())
+    q = torch.full((1, 4, n, D), 8.0).bfloat16().cuda()
+    o, lse = vsa2.attn_cache(cache, q, torch.tensor([m], dtype=torch.int32).cuda(), causal=True)
+    assert (o == 2.0 ** -40).all() and (lse == 512).all()

@@ -569,7 +569,8 @@ vsa2_status vsa2_qk_norm_rope_bwd(const vsa2_problem* p, const vsa2_rope* r, flo
  * table device int32 [batch][table_heads][max_pages]: the pages of each
  *       sequence's list in order; list position j is token j % 64 of page
  *       table[j / 64].  table_heads is 1 (one list for all KV heads) or heads_kv
- *       (every head has its own, as a router that picks pages per head gives).
+ *       (every head has its own, where a caller picks pages per head; no call of
+ *       this library makes such lists).
  *       Entries outside [0, pages) are skipped: nothing is written or read
  *       there, and attention leaves those 64 positions out.
  */

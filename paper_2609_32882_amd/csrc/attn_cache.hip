@@ -22,8 +22,9 @@
 // and the workgroups of a split take different pages of a list, each with its
 // own running maximum and sum, and are joined at the end in a fixed order.  16
 // sequences of 20,000 to 76,800 tokens, 40 query and 8 KV heads of 128: 281 us, 5.7
-// TB/s.  Bound by issue for many rows: 1,792 tokens over 35,840, 12 heads, 410 us,
-// 0.96 PFLOP/s.
+// TB/s.  For many rows bound by vector instructions, which hardly overlap with the
+// MFMAs of two waves a SIMD: 1,792 tokens over 35,840, 12 heads, 430 us, 0.92
+// PFLOP/s; vector unit busy 63% of the cycles and MFMAs 43%, waits for LDS 1%.
 #include <algorithm>
 #include <cfloat>
 
@@ -315,10 +316,10 @@ struct page_walk {
 // The piece of a list, and its row tile, that a workgroup takes.  The tiles of a
 // piece run on one XCD, whose L2 then holds the piece's pages.  Spread: next pieces
 // on next XCDs, so that the long and the short sequences of a batch load all of
-// them alike (16 sequences of 20,000 to 76,800 tokens: 305 us against 332 with
-// neighbouring lists on one XCD, 16 x 8 lists of 200 rows 285 against 342); else a
+// them alike (16 sequences of 20,000 to 76,800 tokens: 287 us against 332 with
+// neighbouring lists on one XCD, 16 x 8 lists of 200 rows 275 against 327); else a
 // run of pieces for every XCD, which keeps a few pieces of many tiles even (12 lists
-// of 1,792 rows: 444 us against 616 spread).
+// of 1,792 rows: 434 us against 590 spread).
 __device__ __forceinline__ uint32_t piece_of(const attn_args& a, int& tile) {
     if (!a.spread) {
         const uint32_t item = static_cast<uint32_t>(xcd_item(blockIdx.x, gridDim.x));
@@ -1096,7 +1097,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
 // each taking every SLICES-th piece, whose sums are added in order: one group
 // (8 rows a workgroup) for up to 8 pieces, eight groups for up to 32, 32 for more,
 // where a group's loads one after the other took longer than the pieces themselves
-// (512 pieces of one row: the whole call 40.5 us with eight groups, 28.5 with 32).
+// (512 pieces of one row: the whole call 41.4 us with eight groups, 29.1 with 32).
 template <typename T, int D, int SLICES>
 __global__ __launch_bounds__(SLICES > 8 ? 32 * SLICES : 256) void attn_cache_join_kernel(attn_args a, int tile_rows) {
     constexpr int RPW = SLICES > 8 ? 1 : 8 / SLICES;       // rows of a workgroup
@@ -1170,20 +1171,23 @@ template <typename T, int D> constexpr bool two_tiles = !(sizeof(T) == 4 && D ==
 // Which kernel: tiles of 16 or 32 rows whose waves share out a list's pages, or
 // 128-row tiles whose waves share the pages.  The first reads and decodes a page
 // once per tile but splits finely; measured over lists of 20,000 tokens (us,
-// small tiles against 128-row ones): bf16, D = 128, 8 lists of 128 rows 27 against
-// 36, 32 of 128 rows 63 against 66, 128 lists of 64 rows 162 against 196, of 96
-// rows 229 against 209; fp32, D = 128, 32 lists of 128 rows 124 against 124.
+// tiles of 16 and of 32 against 128-row ones): bf16, D = 128, 8 lists of 128 rows
+// 33 and 31 against 42, 32 of 96 rows 68 and 55 against 65, of 128 rows 94 and 72
+// against 72, 128 lists of 64 rows 193 and 154 against 196, of 96 rows 264 and 201
+// against 204; fp32, D = 128, 32 lists of 128 rows 131 against 127.  fp32 at D = 64
+// would gain from pairs also at 128 lists of 96 rows (lists of uneven lengths 151 and
+// 138 against 170), which the limit of 64 lists, drawn for D = 128, leaves out.
 bool takes_tiles(int dtype, int D, int64_t lists, int64_t rows) {
     return rows <= 64 || (rows <= 128 && ((dtype == 0 && D == 128) || lists < 64));
 }
 
 // Small tiles of 32 rows: half the decoding, where there are workgroups enough
 // either way.  Measured with 128 lists (us, 16 rows against 32): lists of 40,000
-// tokens, bf16, D = 128, 32 / 48 / 64 rows 247 / 346 / 382 against 246 / 290 / 308;
-// D = 64 136 / 169 / 206 against 133 / 187 / 190 (a half-empty pair costs more than
-// it saves there); 5,000 tokens 27 / 32 / 33 against 30 / 33 / 34.  Of short
+// tokens, bf16, D = 128, 32 / 48 / 64 rows 248 / 325 / 366 against 250 / 271 / 280;
+// D = 64 140 / 173 / 212 against 135 / 183 / 187 (a half-empty pair costs more than
+// it saves there); 5,000 tokens 35 / 44 / 44 against 36 / 42 / 42.  Of short
 // lists, where a pair makes the tiles one and the call one launch: 32 rows of 1,000
-// tokens 16.6 against 14.6.
+// tokens 16.3 against 15.0.
 bool takes_pairs(int dtype, int D, int64_t lists, int64_t rows, int pages) {
     const int64_t tiles = (rows + TILE - 1) / TILE;
     if (tiles == 1 || (dtype == 0 && D == 128) || lists * tiles < 128) return false;
@@ -1200,9 +1204,13 @@ attn_plan plan_attn(int dtype, int D, const cache_view& c, int heads_q, int n) {
         // A list in one piece takes eight waves that join it without a second
         // launch: short ones, and those of many sequences up to 200 pages.  One
         // token, in one piece against several (us): 12 lists of 1,792 tokens, bf16
-        // 10.5 against 10.9, fp32 (D = 128) 13.7 against 11.4; 128 lists of 4,000,
-        // bf16 24.5 against 29.5, fp32 30.0 against 29.4; 192 of 6,000, bf16 47
-        // against 54, fp32 51 against 55.
+        // 10.9 against 11.1, fp32 (D = 128) 14.0 against 11.3; 128 lists of 4,000,
+        // bf16 24.8 against 28.5 (uneven lengths 21.0 against 23.3), fp32 29.0
+        // against 30.2 (28.1 against 24.5); 192 of 6,000, bf16 48 against 56 (36
+        // against 37), fp32 50 against 59 (41 against 41).  Near 200 pages uneven
+        // lengths lose: 128 of up to 12,000, bf16, D = 128 79 against 78, uneven 55
+        // against 48, D = 64 37 against 38 and 36 against 29; 192, fp32, D = 64 52
+        // against 44.
         const int one = lists >= (dtype == 1 ? 128 : 192) ? 200 : (dtype == 0 && D == 128 && lists < 128 ? 16 : 32);
         if (p.tiles == 1 && c.max_pages <= one) {
             p.waves = 8;
@@ -1211,10 +1219,14 @@ attn_plan plan_attn(int dtype, int D, const cache_view& c, int heads_q, int n) {
         }
         // Else the 512 workgroups of four waves that are resident at once (D = 128),
         // and a page for every wave at least; 256 where the pieces of few rows take
-        // longer to join than they save (one token over 200,000: 512 workgroups 28
-        // us, 256 22); 1,024 where many sequences are of different lengths and the
-        // pieces stay long (16 x 8 lists of 20,000 to 76,800 tokens: 512 workgroups
-        // 305 us, 1,024 286, 2,048 336).
+        // longer to join than they save (one token over 200,000: 512 workgroups 29
+        // us, 256 23); 1,024 from 128 lists on, where the lengths, which only the GPU
+        // knows, may be uneven and the pieces stay long.  One token over up to 40,000,
+        // D = 128, 512 workgroups against 1,024 (us; even, uneven lengths): 96 lists
+        // 176, 122 against 187, 121; 112 205, 142 against 206, 137; 128 232, 159
+        // against 232, 155; 160 285, 193 against 287, 189; 256 443, 298 against 450,
+        // 289; D = 64, 96 lists 94, 63 against 102, 60, 128 119, 88 against 125, 86.
+        // 16 x 8 lists of 20,000 to 76,800: 299 against 287, 2,048 287.
         p.waves = 4;
         const int64_t items = lists * p.tiles, most = (c.max_pages + 3) / 4, pages64 = c.max_pages / 64;
         int64_t want = (dtype == 1 && p.tiles == 1 && items <= 16 ? 256 : 512) / items;

@@ -1,8 +1,8 @@
 // Writing tokens into the paged 8-bit key/value cache and reading them back.
 //
 // Bound by memory: a value comes in 2 or 4 bytes and goes out in one (or the
-// reverse).  A workgroup takes one page of one KV head.  Its 16 groups of D/8
-// lanes each take four neighbouring tokens 16 t + 4 g .. + 3 (a dword of codes
+// reverse).  A workgroup takes one page of one KV head, in a write its keys or its
+// values.  Its 16 groups of D/8 lanes each take four neighbouring tokens 16 t + 4 g .. + 3 (a dword of codes
 // per element of V), with a row's 8 elements in each lane; the page goes through
 // LDS in its own order, so both sides of the copy are whole lines although K's
 // and V's elements change places.

@@ -14,8 +14,9 @@
 // result's own rounding.  fp16's exponents do not reach far: P is scaled by a
 // power of two that makes the largest power seen 2^7, and in rows whose weight is
 // on tokens of much smaller powers by one more (row_softmax).  Measured against
-// bf16 P: 2.5% of the time at 1,792 rows, 3 to 9% over a few rows where codes and
-// weights bound a page (D = 64), none where memory does.
+// bf16 P: 3% of the time at 1,792 rows, 3 to 9% over a few rows where codes and
+// weights bound a page (D = 64), none where memory does; where every page holds
+// powers 2^7 apart or more, 17 to 26% there.
 //
 // Bound by memory for single tokens: 2 (D + 1) bytes per token and KV head.  A
 // page is 16 KB in runs of 1 KB per load instruction; the waves of a workgroup
@@ -235,34 +236,40 @@ struct row_softmax {
 template <typename T> constexpr bool lifted_of = sizeof(T) == 2;
 template <typename T> using row_softmax_t = row_softmax<lifted_of<T>>;
 
-// The exponents (+ 127) of a wave's powers, the same in every lane: the largest so far (E), what it
-// was before the page at hand, and whether some token of the page lies more than 2^7 below.
+// The exponents (+ 127) of a wave's powers, the same in every lane: the largest so far (E) and what
+// it was before the page at hand.  Of the page (or pages) at hand a lane has four bytes, all lanes
+// together all of them; `marked` holds the bytes that count, the others 0.
 struct powers_seen {
     int most = 0, was = 0;
-    bool wide = false;
-    // Is one of the marked bytes of four powers above E, or more than 2^7 below?
-    __device__ __forceinline__ bool news(uint32_t four, uint32_t marked) const {
-        return ((four - static_cast<uint32_t>(most - 7) * 0x01010101u) & 0xf8f8f8f8u & marked) != 0;
+    // Is one of the marked bytes above E, or more than 2^7 below?
+    __device__ __forceinline__ bool news(uint32_t four, uint32_t mask) const {
+        return ((four - static_cast<uint32_t>(most - 7) * 0x01010101u) & 0xf8f8f8f8u & mask) != 0;
     }
-    // `marked`: those of the page's (or pages') in every lane, all of them together; the others 0.
-    __device__ __forceinline__ void look(uint32_t marked) {
-        const uint32_t ev = max(marked & 0xffu, (marked >> 8) & 0xffu), od = max((marked >> 16) & 0xffu, marked >> 24);
-        float x = static_cast<float>(max(ev, od));
-        x = fmaxf(x, dpp_f32<0xB1>(x));
-        x = fmaxf(x, dpp_f32<0x4E>(x));
-        x = fmaxf(x, dpp_f32<0x141>(x));
-        x = fmaxf(x, dpp_f32<0x140>(x));
-        was = most;
-        most = max(most, __builtin_amdgcn_readfirstlane(static_cast<int>(groups_max(x))));
+    // Is one more than 2^by below E?  In any lane.
+    __device__ __forceinline__ bool below(uint32_t marked, int by) const {
         bool less = false;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int byte = static_cast<int>((marked >> (8 * i)) & 0xffu);
-            less |= byte != 0 && byte < most - 7;
+            less |= byte != 0 && byte < most - by;
         }
-        wide = __ballot(less) != 0;
+        return __ballot(less) != 0;
     }
-    // 2^(power - E + 7), of a byte that raised() gave where the powers are wide
+    // Brings E up to date; does it change?
+    __device__ __forceinline__ bool look(uint32_t marked) {
+        const uint32_t ev = max(marked & 0xffu, (marked >> 8) & 0xffu), od = max((marked >> 16) & 0xffu, marked >> 24);
+        const int top = static_cast<int>(max(ev, od));
+        was = most;
+        if (__ballot(top > most) == 0) return false;
+        float x = static_cast<float>(top);
+        x = fmaxf(x, dpp_f32<0xB1>(x));
+        x = fmaxf(x, dpp_f32<0x4E>(x));
+        x = fmaxf(x, dpp_f32<0x141>(x));
+        x = fmaxf(x, dpp_f32<0x140>(x));
+        most = __builtin_amdgcn_readfirstlane(static_cast<int>(groups_max(x)));
+        return true;
+    }
+    // 2^(power - E + 7), of a byte that raised() gave where some are more than 2^134 below
     __device__ __forceinline__ float scaled(uint32_t byte) const {
         return __uint_as_float((byte << 23) + (static_cast<uint32_t>(134 - most) << 23));
     }
@@ -402,7 +409,8 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
     uint32_t marked = ~0u;
     if constexpr (MASKED) marked = first_bytes(lim_max - (pos + 16 * at + 4 * g));
     float mx[XT];
-    bool far = NT == 1 && seen.news(four, marked);
+    const bool news = NT == 1 && seen.news(four, marked);
+    bool far = false;
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         if constexpr (MASKED) {
@@ -422,10 +430,11 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
     }
     // the running maxima move only when one would grow by more than 8 (weights
     // up to 2^8 of the first), less with a lift: most pages leave O alone
-    if (__ballot(far) != 0) {
+    if (__ballot(far || news) != 0) {
+        bool moves = __ballot(far) != 0;
         if constexpr (NT == 1) {
-            seen.look(four & marked);
-            if (seen.wide) {
+            moves |= seen.look(four & marked);
+            if (seen.below(four & marked, 134)) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     uint32_t w = 0;
@@ -435,12 +444,14 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
                 }
             }
         }
+        const bool wide = NT == 1 && moves && seen.below(four & marked, 7);
 #pragma unroll
         for (int x = 0; x < XT; ++x) {
+            if (!moves) continue;
             row_softmax_t<T>& w = st[x].w;
             const float up = fmaxf(w.base + w.lift(), mx[x] * scale);
             float most = fmaf(mx[x], scale, -up) - 7.f;
-            if (NT == 1 && seen.wide) {
+            if (wide) {
                 most = -INFINITY;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
@@ -716,7 +727,13 @@ __device__ __forceinline__ void rows_move(const f32x16_t (&s)[N], const float (*
     if (__ballot(far) == 0) return;
     const float up = fmaxf(st.w.base + st.w.lift(), mx * scale);
     float most = fmaf(mx, scale, -up) - 7.f;
-    if (LIFTED && seen.wide) {
+    bool wide = false;          // a lane's token of each page more than 2^7 below E (past a limit: whatever)
+    if constexpr (LIFTED) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) wide |= power[i][1][lane_id()] < 1.f;
+        wide = __ballot(wide) != 0;
+    }
+    if (wide) {
         const int h2 = lane_id() >> 5;
         most = -INFINITY;
 #pragma unroll
@@ -1006,16 +1023,11 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 4 ? 1 : 2) void attn_cache_ro
     int at[STAGE];
     auto turn = [&]() {
         if constexpr (NT == 1) {
-            uint32_t powers = 0, marked = 0;
+            uint32_t marked = 0;
 #pragma unroll
-            for (int x = 0; x < STAGE; ++x) {
-                const uint32_t here = x < have && pos[x] * CACHE_TOKENS + lane < wmax ? 0xffu << (8 * x) : 0u;
-                powers |= static_cast<uint32_t>(ve[x]) << (8 * x);
-                marked |= here;
-            }
-            seen.was = seen.most;
-            seen.wide = false;
-            if (__ballot(seen.news(powers, marked)) != 0) seen.look(powers & marked);
+            for (int x = 0; x < STAGE; ++x)
+                if (x < have && pos[x] * CACHE_TOKENS + lane < wmax) marked |= static_cast<uint32_t>(ve[x]) << (8 * x);
+            seen.look(marked);
         }
 #pragma unroll
         for (int x = 0; x < STAGE; ++x) {

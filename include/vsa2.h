@@ -641,6 +641,111 @@ vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q,
                             float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * vsa2_attn_cache_shared - vsa2_attn_cache where several sequences go on from one
+ * list: sequence b of c attends list b / (c->batch / prefix->batch) of prefix first,
+ * up to prefix_length, then its own.  One softmax over both:
+ *   seen by token i of sequence b: prefix positions j < prefix_length[b / samples]
+ *   and own positions j < limit, limit as in vsa2_attn_cache (causal there, too);
+ *   nothing for i >= count[b].
+ * The shared list is read and decoded once for tiles of the rows of all its
+ * sequences.
+ *   prefix  lists of prefix->batch groups, a divisor of c->batch; heads_kv and head_dim as
+ *           c's; its pool may be c's or another.
+ *   prefix_length  device int32 [prefix->batch]; length, count  as in vsa2_attn_cache.
+ *   ws, ws_bytes  workspace of vsa2_attn_cache_shared_workspace bytes, 256-byte aligned.
+ * Types, q, o, lse, roundings and what masked places reach are as for vsa2_attn_cache.
+ * Errors: as for vsa2_attn_cache; groups that do not divide the batch, other heads or
+ * head sizes (VSA2_ERR_SHAPE); more than 2^30 rows of one shared list
+ * (VSA2_ERR_UNSUPPORTED).
+ */
+vsa2_status vsa2_attn_cache_shared_workspace(const vsa2_cache* prefix, const vsa2_cache* c, int32_t heads_q, int32_t n,
+                                             size_t* bytes);
+vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n,
+                                   const vsa2_rows* q, const int32_t* prefix_length, const int32_t* length,
+                                   const int32_t* count, int32_t causal, const vsa2_rows* o, float* lse, void* ws,
+                                   size_t ws_bytes, hipStream_t stream);
+
+/*
+ * vsa2_attn_cache_scored - vsa2_attn_cache with other scores and fewer positions.
+ * With p = length[b] - count[b] + i, the list position of token i itself, and
+ * x = q.k_j / sqrt(D), the softmax is over
+ *   y = cap tanh(x / cap) - slope[h] |p - j|        (cap = 0: x; slope NULL: none)
+ * of the positions j < limit (as in vsa2_attn_cache) with
+ *   j < sink,  or  j > p - window  and  span[b][i][0] <= j < span[b][i][1]
+ * (window = 0, span NULL: all).  A window behind some first tokens; documents, each
+ * token's own [from, to); a prefix that sees itself whole, [0, max(prefix, p + 1)) with
+ * causal = 0.  The window also ends lists that lose their oldest pages: pages that no row
+ * sees are not visited.
+ *   slope   device fp32 [heads_q], finite, or NULL.
+ *   span    device int32 [batch][n][2] or NULL.
+ *   The rest is as for vsa2_attn_cache, what positions hold that no row sees reaches
+ *   no output.  ws: vsa2_attn_cache_scored_workspace bytes for the same scores.
+ * Errors: as for vsa2_attn_cache; cap, window or sink negative, cap not finite
+ * (VSA2_ERR_VALUE).
+ */
+typedef struct {
+    float cap;
+    int32_t window, sink;
+    const float* slope;
+    const int32_t* span;
+} vsa2_scores;
+vsa2_status vsa2_attn_cache_scored_workspace(const vsa2_cache* c, const vsa2_scores* scores, int32_t heads_q, int32_t n,
+                                             size_t* bytes);
+vsa2_status vsa2_attn_cache_scored(const vsa2_cache* c, const vsa2_scores* scores, int32_t dtype, int32_t heads_q, int32_t n,
+                                   const vsa2_rows* q, const int32_t* length, const int32_t* count, int32_t causal,
+                                   const vsa2_rows* o, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * vsa2_cache_assign - every sequence's page list becomes the first tokens of its own
+ * or another's, with room for new ones: lists are forked, cut, freed and extended, whole
+ * pages leave them, and a shared last page is copied before it is written, all on the
+ * GPU.  refs[p] says how many list entries name page p (all lists of all tables of the
+ * pool); 0: free.  With `old` the lists before the call, M = max_pages and, for sequence b,
+ *   src  = source[b] (b without source); len = length[b] in [0, 64 M], 0 where src is
+ *          outside [0, batch);  P = ceil(len / 64);  (first, num) = drop[b], num at least 0
+ * the lists become, all at once,
+ *   new[b][s] = old[src][s + (s >= first ? num : 0)] for s < P; -1 behind, past M, and for
+ *          entries that name no page,
+ * and refs follows.  Then, b ascending, pages are asked for:
+ *   - if count[b] > 0, len % 64 > 0 and refs of the page new[b][P - 1] is above 1: one for a
+ *     copy of that page (all KV heads, all bytes), which takes its place;
+ *   - for each s from P to min(M, ceil((len + count[b]) / 64)) - 1: new[b][s].
+ * Each gets the free page of the lowest index, and refs 1; none is left: -1, and a page that
+ * could not be copied stays shared.  room[b] = how many of the count[b] tokens have a place
+ * that is the sequence's alone: the count to give vsa2_cache_write with start = length.
+ *   c       the cache; c->table is `table`, table_heads is 1.  pool: copied pages are written.
+ *   table   device int32 [batch][max_pages], read and written.
+ *   refs    device int32 [pages], 16-byte aligned, read and written.  A new pool: zeros, and
+ *           a table of -1.  Lists that a caller keeps in other tables (a shared prefix) count
+ *           there as well.
+ *   length  device int32 [batch], after the drop;  source, count  device int32 [batch] or NULL;
+ *   drop    device int32 [batch][2] or NULL;  room  device int32 [batch] or NULL.
+ *   ws, ws_bytes  workspace of vsa2_cache_assign_workspace bytes, 256-byte aligned.
+ * Errors: NULL pointers, shapes as for vsa2_cache_write; table_heads above 1 (VSA2_ERR_SHAPE);
+ * table other than c->table (VSA2_ERR_VALUE); batch * (max_pages + 1) of 2^31 or more, batch
+ * of 2^24 or more, more than 32,768 KV heads (VSA2_ERR_UNSUPPORTED); misalignment; workspace.
+ */
+vsa2_status vsa2_cache_assign_workspace(const vsa2_cache* c, size_t* bytes);
+vsa2_status vsa2_cache_assign(const vsa2_cache* c, int32_t* table, int32_t* refs, const int32_t* length,
+                              const int32_t* source, const int32_t* drop, const int32_t* count, int32_t* room, void* ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/*
+ * vsa2_cache_copy - tokens as they are stored (codes and powers) from one cache's lists
+ * into another's: token i < min(n, count[b]) of sequence b is position index[b][i] of
+ * list b of `from` and goes to position start[b] + i of list b of `to`.  Positions that
+ * `from` lacks read as zeros; positions that `to` lacks are skipped; the rest of its
+ * pages keeps what it holds.
+ *   from, to  equal batch, heads_kv and head_dim; one pool or two.  No page that the call
+ *           writes may be one that it reads.
+ *   index   device int32 [batch][n];  start  device int32 [batch];  count  device int32
+ *           [batch], or NULL for n.
+ * Errors: as for vsa2_cache_write; unlike caches (VSA2_ERR_SHAPE).  n = 0 does nothing.
+ */
+vsa2_status vsa2_cache_copy(const vsa2_cache* from, const vsa2_cache* to, int32_t n, const int32_t* index,
+                            const int32_t* start, const int32_t* count, hipStream_t stream);
+
+/*
  * vsa2_mfma_peak_probe - a measurement aid, not part of the attention path:
  * the dense bf16 MFMA rate this GPU reaches, the measured counterpart of the
  * published peak the attention kernels are rated against.  Launches one

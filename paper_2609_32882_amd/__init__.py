@@ -36,6 +36,9 @@ EXPORTS = ("vsa2_status_str", "vsa2_pool", "vsa2_route_capacity", "vsa2_route_wo
            "vsa2_qk_norm_rope", "vsa2_qk_norm_rope_workspace", "vsa2_qk_norm_rope_bwd",
            "vsa2_cache_page_bytes", "vsa2_cache_write", "vsa2_cache_read",
            "vsa2_attn_cache_workspace", "vsa2_attn_cache",
+           "vsa2_attn_cache_shared_workspace", "vsa2_attn_cache_shared",
+           "vsa2_attn_cache_scored_workspace", "vsa2_attn_cache_scored",
+           "vsa2_cache_assign_workspace", "vsa2_cache_assign", "vsa2_cache_copy",
            "vsa2_mfma_peak_probe", "vsa2_dq_atomic_probe")
 
 
@@ -64,6 +67,11 @@ class vsa2_cache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("batch", "heads_kv", "head_dim", "pages", "max_pages", "table_heads")] + \
                [("pool", ctypes.c_void_p), ("table", ctypes.c_void_p)]
+
+
+class vsa2_scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32), ("sink", ctypes.c_int32),
+                ("slope", ctypes.c_void_p), ("span", ctypes.c_void_p)]
 
 
 class Vsa2Error(RuntimeError):
@@ -116,6 +124,14 @@ def _lib():
         L.vsa2_cache_read.argtypes = [pc, i32, i32, pw, pw, P, P, P]
         L.vsa2_attn_cache_workspace.argtypes = [pc, i32, i32, ctypes.POINTER(sz)]
         L.vsa2_attn_cache.argtypes = [pc, i32, i32, i32, pw, P, P, i32, pw, P, P, sz, P]
+        L.vsa2_attn_cache_shared_workspace.argtypes = [pc, pc, i32, i32, ctypes.POINTER(sz)]
+        L.vsa2_attn_cache_shared.argtypes = [pc, pc, i32, i32, i32, pw, P, P, P, i32, pw, P, P, sz, P]
+        pq = ctypes.POINTER(vsa2_scores)
+        L.vsa2_attn_cache_scored_workspace.argtypes = [pc, pq, i32, i32, ctypes.POINTER(sz)]
+        L.vsa2_attn_cache_scored.argtypes = [pc, pq, i32, i32, i32, pw, P, P, i32, pw, P, P, sz, P]
+        L.vsa2_cache_assign_workspace.argtypes = [pc, ctypes.POINTER(sz)]
+        L.vsa2_cache_assign.argtypes = [pc, P, P, P, P, P, P, P, P, sz, P]
+        L.vsa2_cache_copy.argtypes = [pc, pc, i32, P, P, P, P]
         L.vsa2_mfma_peak_probe.argtypes = [i32, P, ctypes.POINTER(i64), P]
         L.vsa2_dq_atomic_probe.argtypes = [pp, P, P, i64, P, P]
         for n in EXPORTS[1:]:
@@ -293,6 +309,43 @@ def vsa2_attn_cache_workspace(c, heads_q, n):
 def vsa2_attn_cache(c, dtype, heads_q, n, q, length, count, causal, o, lse, ws, ws_bytes, stream=0):
     return _lib().vsa2_attn_cache(_ref(c), dtype, heads_q, n, _ref(q), length, count, causal, _ref(o), lse, ws,
                                   ws_bytes, stream)
+
+
+def vsa2_attn_cache_shared_workspace(prefix, c, heads_q, n):
+    b = ctypes.c_size_t(0)
+    st = _lib().vsa2_attn_cache_shared_workspace(_ref(prefix), _ref(c), heads_q, n, ctypes.byref(b))
+    return st, b.value
+
+
+def vsa2_attn_cache_shared(prefix, c, dtype, heads_q, n, q, prefix_length, length, count, causal, o, lse, ws, ws_bytes,
+                           stream=0):
+    return _lib().vsa2_attn_cache_shared(_ref(prefix), _ref(c), dtype, heads_q, n, _ref(q), prefix_length, length, count,
+                                         causal, _ref(o), lse, ws, ws_bytes, stream)
+
+
+def vsa2_attn_cache_scored_workspace(c, scores, heads_q, n):
+    b = ctypes.c_size_t(0)
+    st = _lib().vsa2_attn_cache_scored_workspace(_ref(c), _ref(scores), heads_q, n, ctypes.byref(b))
+    return st, b.value
+
+
+def vsa2_attn_cache_scored(c, scores, dtype, heads_q, n, q, length, count, causal, o, lse, ws, ws_bytes, stream=0):
+    return _lib().vsa2_attn_cache_scored(_ref(c), _ref(scores), dtype, heads_q, n, _ref(q), length, count, causal, _ref(o),
+                                         lse, ws, ws_bytes, stream)
+
+
+def vsa2_cache_assign_workspace(c):
+    b = ctypes.c_size_t(0)
+    st = _lib().vsa2_cache_assign_workspace(_ref(c), ctypes.byref(b))
+    return st, b.value
+
+
+def vsa2_cache_assign(c, table, refs, length, source, drop, count, room, ws, ws_bytes, stream=0):
+    return _lib().vsa2_cache_assign(_ref(c), table, refs, length, source, drop, count, room, ws, ws_bytes, stream)
+
+
+def vsa2_cache_copy(src, dst, n, index, start, count, stream=0):
+    return _lib().vsa2_cache_copy(_ref(src), _ref(dst), n, index, start, count, stream)
 
 
 # --------------------------------------------------------------------------
@@ -717,3 +770,38 @@ def attn_cache(cache, q, length, count=None, causal=False, o=None):
     count[b] (None: n) of them and see no later one.  Returns (o, lse), o like q
     and contiguous unless given, lse [batch, heads_q, n] fp32."""
     return _marshal().attn_cache(cache.c, q, length, count, True if causal else False, o, _stream, cache.device)
+
+
+def attn_cache_shared(prefix, cache, q, prefix_length, length, count=None, causal=False, o=None):
+    """attn_cache where several sequences go on from one list: sequence b of `cache`
+    attends the first prefix_length (int32 [groups]) positions of list
+    b // (batch / groups) of the KVCache `prefix`, then its own first length[b]
+    (causal among those).  The shared list is read once for all its sequences."""
+    return _marshal().attn_cache_shared(prefix.c, cache.c, q, prefix_length, length, count, True if causal else False, o,
+                                        _stream, prefix.device, cache.device)
+
+
+def attn_cache_scored(cache, q, length, count=None, causal=False, cap=0.0, slope=None, window=0, sink=0, span=None, o=None):
+    """attn_cache with scores cap * tanh(x / cap) - slope[h] * |p - j| (cap 0: x; slope
+    fp32 [heads_q] or None) over positions j < sink, or within the window j > p - window
+    (0: all) and the token's own range span[b, i] = [from, to) (int32 [batch, n, 2] or
+    None); p = length[b] - count[b] + i is the token's own position."""
+    return _marshal().attn_cache_scored(cache.c, q, length, count, True if causal else False, cap, slope, window, sink, span,
+                                        o, _stream, cache.device)
+
+
+def cache_assign(cache, refs, length, source=None, drop=None, count=None, room=None):
+    """New page lists for all sequences, in cache.table: the first length[b] tokens of list
+    source[b] (None: its own; -1: an empty list) without the pages drop[b] = (first,
+    number), and pages for count[b] more tokens (None: none).  A last page that is shared
+    and will be written is copied.  refs int32 [pages] says how many entries name each
+    page (a new pool: zeros, and a table of -1) and follows.  Returns room int32 [batch]:
+    how many of the count[b] tokens have a place, the count for cache_write."""
+    return _marshal().cache_assign(cache.c, cache.table, refs, length, source, drop, count, room, _stream, cache.device)
+
+
+def cache_copy(src, dst, index, start, count=None):
+    """Tokens as they are stored, from one KVCache's lists into another's: position
+    index[b, i] (int32 [batch, n]) of src's list b goes to position start[b] + i of dst's
+    list b, i < count[b] (None: all n); no page may be both read and written."""
+    _marshal().cache_copy(src.c, dst.c, index, start, count, _stream, src.device, dst.device)

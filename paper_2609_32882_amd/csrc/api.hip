@@ -222,6 +222,17 @@ vsa2_status cache_copy(bool write, const vsa2_cache* c, int32_t dtype, int32_t n
     return VSA2_OK;
 }
 
+// Lists that can be assigned: one for all KV heads.
+vsa2_status check_lists(const vsa2_cache* c, vsa2::cache_view* v) {
+    const vsa2_status st = check_cache(c, VSA2_BF16, 0, v);
+    if (st != VSA2_OK) return st;
+    if (c->table_heads != 1) return VSA2_ERR_SHAPE;
+    // requests are numbered in 32 bits; a copied page's 16 KB pieces are a launch's second axis
+    if (c->batch > kMaxWorkgroups || static_cast<int64_t>(c->batch) * (c->max_pages + 1) > INT32_MAX || c->heads_kv > 32768)
+        return VSA2_ERR_UNSUPPORTED;
+    return VSA2_OK;
+}
+
 // What attention over the cache and its workspace query check alike.
 vsa2_status check_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n, vsa2::cache_view* view) {
     const vsa2_status st = check_cache(c, dtype, n, view);
@@ -232,6 +243,26 @@ vsa2_status check_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q
     if (group * n > (int64_t(1) << 30)) return VSA2_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(c->batch) * c->heads_kv > kMaxWorkgroups / 4 / (group * n / 16 + 1))
         return VSA2_ERR_UNSUPPORTED;
+    return VSA2_OK;
+}
+
+// What attention over a shared list and its workspace query check alike: the shared rows, too.
+vsa2_status check_attn_shared(const vsa2_cache* pre, const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n,
+                              vsa2::cache_view* pre_view, vsa2::cache_view* view) {
+    vsa2_status st = check_attn_cache(c, dtype, heads_q, n, view);
+    if (st != VSA2_OK) return st;
+    if ((st = check_cache(pre, dtype, n, pre_view)) != VSA2_OK) return st;
+    if (pre->heads_kv != c->heads_kv || pre->head_dim != c->head_dim || c->batch % pre->batch) return VSA2_ERR_SHAPE;
+    const int64_t rows = static_cast<int64_t>(heads_q / c->heads_kv) * n, samples = c->batch / pre->batch;
+    if (rows * samples > (int64_t(1) << 30)) return VSA2_ERR_UNSUPPORTED;
+    return VSA2_OK;
+}
+
+// The options of a scored call.
+vsa2_status check_scores(const vsa2_scores* s) {
+    if (!s) return VSA2_ERR_NULL;
+    if (!(s->cap >= 0.f) || s->cap > 3.402823466e38f) return VSA2_ERR_VALUE;
+    if (s->window < 0 || s->sink < 0) return VSA2_ERR_VALUE;
     return VSA2_OK;
 }
 
@@ -762,6 +793,112 @@ vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q,
     if (need && reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
     VSA2_TRY_HIP(vsa2::launch_attn_cache(dtype, c->head_dim, view, heads_q, n, view_of(q), length, count, causal != 0,
                                          view_of(o), lse, ws, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_attn_cache_shared_workspace(const vsa2_cache* prefix, const vsa2_cache* c, int32_t heads_q, int32_t n,
+                                             size_t* bytes) {
+    vsa2::cache_view pre, view;
+    const vsa2_status st = check_attn_shared(prefix, c, VSA2_F32, heads_q, n, &pre, &view);
+    if (st != VSA2_OK) return st;
+    if (!bytes) return VSA2_ERR_NULL;
+    *bytes = n == 0 ? 0 : align_up(vsa2::attn_cache_shared_workspace_bytes(pre, view, c->head_dim, heads_q, n));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c, int32_t dtype, int32_t heads_q, int32_t n,
+                                   const vsa2_rows* q, const int32_t* prefix_length, const int32_t* length,
+                                   const int32_t* count, int32_t causal, const vsa2_rows* o, float* lse, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+    vsa2::cache_view pre, view;
+    vsa2_status st = check_attn_shared(prefix, c, dtype, heads_q, n, &pre, &view);
+    if (st != VSA2_OK) return st;
+    if (n == 0) return VSA2_OK;
+    if ((st = check_cache_memory(prefix)) != VSA2_OK) return st;
+    if ((st = check_cache_memory(c)) != VSA2_OK) return st;
+    if (!prefix_length || !length || !lse) return VSA2_ERR_NULL;
+    if ((st = check_rows(q, dtype, c->batch, heads_q, n, false)) != VSA2_OK) return st;
+    if ((st = check_rows(o, dtype, c->batch, heads_q, n, true)) != VSA2_OK) return st;
+    const size_t need = align_up(vsa2::attn_cache_shared_workspace_bytes(pre, view, c->head_dim, heads_q, n));
+    if (!ws || ws_bytes < need) return VSA2_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
+    VSA2_TRY_HIP(vsa2::launch_attn_cache_shared(dtype, c->head_dim, pre, view, heads_q, n, view_of(q), prefix_length, length,
+                                                count, causal != 0, view_of(o), lse, ws, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_attn_cache_scored_workspace(const vsa2_cache* c, const vsa2_scores* scores, int32_t heads_q, int32_t n,
+                                             size_t* bytes) {
+    vsa2::cache_view view;
+    vsa2_status st = check_attn_cache(c, VSA2_F32, heads_q, n, &view);
+    if (st != VSA2_OK) return st;
+    if ((st = check_scores(scores)) != VSA2_OK) return st;
+    if (!bytes) return VSA2_ERR_NULL;
+    *bytes = n == 0 ? 0 : align_up(vsa2::attn_cache_scored_workspace_bytes(view, c->head_dim, heads_q, n, scores->window,
+                                                                           scores->sink));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_attn_cache_scored(const vsa2_cache* c, const vsa2_scores* scores, int32_t dtype, int32_t heads_q, int32_t n,
+                                   const vsa2_rows* q, const int32_t* length, const int32_t* count, int32_t causal,
+                                   const vsa2_rows* o, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+    vsa2::cache_view view;
+    vsa2_status st = check_attn_cache(c, dtype, heads_q, n, &view);
+    if (st != VSA2_OK) return st;
+    if ((st = check_scores(scores)) != VSA2_OK) return st;
+    if (n == 0) return VSA2_OK;
+    if ((st = check_cache_memory(c)) != VSA2_OK) return st;
+    if (!length || !lse) return VSA2_ERR_NULL;
+    if ((st = check_rows(q, dtype, c->batch, heads_q, n, false)) != VSA2_OK) return st;
+    if ((st = check_rows(o, dtype, c->batch, heads_q, n, true)) != VSA2_OK) return st;
+    const size_t need =
+        align_up(vsa2::attn_cache_scored_workspace_bytes(view, c->head_dim, heads_q, n, scores->window, scores->sink));
+    if (need && (!ws || ws_bytes < need)) return VSA2_ERR_WORKSPACE;
+    if (need && reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
+    const vsa2::score_options options{scores->slope, scores->span, scores->window, scores->sink, scores->cap};
+    VSA2_TRY_HIP(vsa2::launch_attn_cache_scored(dtype, c->head_dim, view, heads_q, n, view_of(q), length, count, causal != 0,
+                                                options, view_of(o), lse, ws, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_cache_assign_workspace(const vsa2_cache* c, size_t* bytes) {
+    vsa2::cache_view view;
+    const vsa2_status st = check_lists(c, &view);
+    if (st != VSA2_OK) return st;
+    if (!bytes) return VSA2_ERR_NULL;
+    *bytes = align_up(vsa2::cache_assign_workspace_bytes(view));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_cache_assign(const vsa2_cache* c, int32_t* table, int32_t* refs, const int32_t* length,
+                              const int32_t* source, const int32_t* drop, const int32_t* count, int32_t* room, void* ws,
+                              size_t ws_bytes, hipStream_t stream) {
+    vsa2::cache_view view;
+    vsa2_status st = check_lists(c, &view);
+    if (st != VSA2_OK) return st;
+    if ((st = check_cache_memory(c)) != VSA2_OK) return st;
+    if (!table || !refs || !length) return VSA2_ERR_NULL;
+    if (table != c->table) return VSA2_ERR_VALUE;
+    if (!aligned16(refs)) return VSA2_ERR_ALIGN;
+    if (!ws || ws_bytes < align_up(vsa2::cache_assign_workspace_bytes(view))) return VSA2_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws) % kAlign) return VSA2_ERR_ALIGN;
+    VSA2_TRY_HIP(vsa2::launch_cache_assign(c->head_dim, view, table, refs, length, source, drop, count, room, ws, stream));
+    return VSA2_OK;
+}
+
+vsa2_status vsa2_cache_copy(const vsa2_cache* from, const vsa2_cache* to, int32_t n, const int32_t* index,
+                            const int32_t* start, const int32_t* count, hipStream_t stream) {
+    vsa2::cache_view a, b;
+    vsa2_status st = check_cache(from, VSA2_BF16, n, &a);
+    if (st != VSA2_OK) return st;
+    if ((st = check_cache(to, VSA2_BF16, n, &b)) != VSA2_OK) return st;
+    if (from->batch != to->batch || from->heads_kv != to->heads_kv || from->head_dim != to->head_dim) return VSA2_ERR_SHAPE;
+    if (n == 0) return VSA2_OK;
+    if ((st = check_cache_memory(from)) != VSA2_OK) return st;
+    if ((st = check_cache_memory(to)) != VSA2_OK) return st;
+    if (!index || !start) return VSA2_ERR_NULL;
+    if (static_cast<int64_t>(to->batch) * to->heads_kv > kMaxWorkgroups / (n / 64 + 2)) return VSA2_ERR_UNSUPPORTED;
+    VSA2_TRY_HIP(vsa2::launch_cache_move(to->head_dim, a, b, n, index, start, count, stream));
     return VSA2_OK;
 }
 

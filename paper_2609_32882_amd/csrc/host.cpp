@@ -376,37 +376,146 @@ PyObject* cache_read(PyObject* const* a, Py_ssize_t n) {
     return t;
 }
 
+// The rows of an attention over a cache: q, and o and lse, made where they are not given.
+struct attn_rows {
+    int32_t code, heads, tokens;
+    vsa2_rows q, o;
+    at::Tensor out, lse, ws;
+    PyObject* given;         // the caller's o, or null
+
+    attn_rows(const vsa2_cache& c, PyObject* query, PyObject* output) {
+        const at::Tensor& x = required(query, "q");
+        if (x.dim() != 4 || x.size(1) > INT32_MAX || x.size(2) > INT32_MAX)
+            fail("q: expected [batch, heads_q, n, D], got " + shape_text(x.sizes()));
+        const int64_t shape[4] = {c.batch, x.size(1), x.size(2), c.head_dim};
+        const at::ScalarType dt = x.scalar_type();
+        code = code_of(dt, "q");
+        heads = static_cast<int32_t>(shape[1]);
+        tokens = static_cast<int32_t>(shape[2]);
+        q = rows(x, shape, dt, "q");
+        given = output == Py_None ? nullptr : output;
+        out = given ? required(output, "o") : at::empty(shape, x.options());
+        o = rows(out, shape, dt, "o");
+        lse = at::empty({shape[0], shape[1], shape[2]}, x.options().dtype(at::kFloat));
+    }
+    float* lse_ptr() const { return lse.data_ptr<float>(); }
+    void* workspace(size_t bytes) {
+        if (!bytes) return nullptr;
+        ws = at::empty({static_cast<int64_t>(bytes)}, lse.options().dtype(at::kByte));
+        return ws.data_ptr();
+    }
+    PyObject* results() const {
+        PyObject* t = PyTuple_New(2);
+        if (given) Py_INCREF(given);
+        PyTuple_SET_ITEM(t, 0, given ? given : wrap(out));
+        PyTuple_SET_ITEM(t, 1, wrap(lse));
+        return t;
+    }
+};
+
+const int32_t* per_sequence(PyObject* o, const vsa2_cache& c, const char* name) {
+    return contiguous<int32_t>(tensor(o, name), {c.batch}, at::kInt, name);
+}
+const int32_t* each_sequence(PyObject* o, const vsa2_cache& c, const char* name) {
+    return contiguous<int32_t>(&required(o, name), {c.batch}, at::kInt, name);
+}
+
 // (cache, q, length, count, causal, o, stream, cache's device) -> (o, lse)
 PyObject* attn_cache(PyObject* const* a, Py_ssize_t n) {
     count_args(n, 8);
     filled_here(a[7], "cache");
     const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
-    const at::Tensor& q = required(a[1], "q");
-    if (q.dim() != 4 || q.size(1) > INT32_MAX || q.size(2) > INT32_MAX)
-        fail("q: expected [batch, heads_q, n, D], got " + shape_text(q.sizes()));
-    const int64_t shape[4] = {c.batch, q.size(1), q.size(2), c.head_dim};
-    const at::ScalarType dt = q.scalar_type();
-    const int32_t code = code_of(dt, "q"), heads = static_cast<int32_t>(shape[1]), tokens = static_cast<int32_t>(shape[2]);
-    const vsa2_rows qr = rows(q, shape, dt, "q");
-    const bool given = a[5] != Py_None;
-    const at::Tensor o = given ? required(a[5], "o") : at::empty(shape, q.options());
-    const vsa2_rows orow = rows(o, shape, dt, "o");
-    const at::Tensor lse = at::empty({shape[0], shape[1], shape[2]}, q.options().dtype(at::kFloat));
+    attn_rows r(c, a[1], a[5]);
     size_t bytes = 0;
-    check("vsa2_attn_cache_workspace", vsa2_attn_cache_workspace(&c, heads, tokens, &bytes));
-    at::Tensor ws;
-    if (bytes) ws = at::empty({static_cast<int64_t>(bytes)}, q.options().dtype(at::kByte));
-    const int32_t* length = contiguous<int32_t>(&required(a[2], "length"), {c.batch}, at::kInt, "length");
-    const int32_t* count = contiguous<int32_t>(tensor(a[3], "count"), {c.batch}, at::kInt, "count");
+    check("vsa2_attn_cache_workspace", vsa2_attn_cache_workspace(&c, r.heads, r.tokens, &bytes));
+    void* ws = r.workspace(bytes);
+    const int32_t *length = each_sequence(a[2], c, "length"), *count = per_sequence(a[3], c, "count");
     const hipStream_t s = stream_of(a[6]);
-    check("vsa2_attn_cache",
-          vsa2_attn_cache(&c, code, heads, tokens, &qr, length, count, a[4] == Py_True ? 1 : 0, &orow,
-                          lse.data_ptr<float>(), bytes ? ws.data_ptr() : nullptr, bytes, s));
-    PyObject* t = PyTuple_New(2);
-    if (given) Py_INCREF(a[5]);
-    PyTuple_SET_ITEM(t, 0, given ? a[5] : wrap(o));
-    PyTuple_SET_ITEM(t, 1, wrap(lse));
-    return t;
+    check("vsa2_attn_cache", vsa2_attn_cache(&c, r.code, r.heads, r.tokens, &r.q, length, count, a[4] == Py_True ? 1 : 0, &r.o,
+                                             r.lse_ptr(), ws, bytes, s));
+    return r.results();
+}
+
+// (prefix, cache, q, prefix_length, length, count, causal, o, stream, both devices) -> (o, lse)
+PyObject* attn_cache_shared(PyObject* const* a, Py_ssize_t n) {
+    count_args(n, 11);
+    filled_here(a[9], "prefix");
+    filled_here(a[10], "cache");
+    const vsa2_cache &p = *structure<vsa2_cache>(a[0], "prefix"), &c = *structure<vsa2_cache>(a[1], "cache");
+    attn_rows r(c, a[2], a[7]);
+    size_t bytes = 0;
+    check("vsa2_attn_cache_shared_workspace", vsa2_attn_cache_shared_workspace(&p, &c, r.heads, r.tokens, &bytes));
+    void* ws = r.workspace(bytes);
+    const int32_t *before = each_sequence(a[3], p, "prefix_length"), *length = each_sequence(a[4], c, "length");
+    const int32_t* count = per_sequence(a[5], c, "count");
+    const hipStream_t s = stream_of(a[8]);
+    check("vsa2_attn_cache_shared",
+          vsa2_attn_cache_shared(&p, &c, r.code, r.heads, r.tokens, &r.q, before, length, count, a[6] == Py_True ? 1 : 0, &r.o,
+                                 r.lse_ptr(), ws, bytes, s));
+    return r.results();
+}
+
+// (cache, q, length, count, causal, cap, slope, window, sink, span, o, stream, cache's device) -> (o, lse)
+PyObject* attn_cache_scored(PyObject* const* a, Py_ssize_t n) {
+    count_args(n, 13);
+    filled_here(a[12], "cache");
+    const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
+    attn_rows r(c, a[1], a[10]);
+    vsa2_scores sc;
+    sc.cap = static_cast<float>(real(a[5]));
+    sc.slope = contiguous<float>(tensor(a[6], "slope"), {r.heads}, at::kFloat, "slope");
+    sc.window = integer32(a[7], "window");
+    sc.sink = integer32(a[8], "sink");
+    sc.span = contiguous<int32_t>(tensor(a[9], "span"), {c.batch, r.tokens, 2}, at::kInt, "span");
+    size_t bytes = 0;
+    check("vsa2_attn_cache_scored_workspace", vsa2_attn_cache_scored_workspace(&c, &sc, r.heads, r.tokens, &bytes));
+    void* ws = r.workspace(bytes);
+    const int32_t *length = each_sequence(a[2], c, "length"), *count = per_sequence(a[3], c, "count");
+    const hipStream_t s = stream_of(a[11]);
+    check("vsa2_attn_cache_scored",
+          vsa2_attn_cache_scored(&c, &sc, r.code, r.heads, r.tokens, &r.q, length, count, a[4] == Py_True ? 1 : 0, &r.o,
+                                 r.lse_ptr(), ws, bytes, s));
+    return r.results();
+}
+
+// (cache, table, refs, length, source, drop, count, room, stream, cache's device) -> room
+PyObject* cache_assign(PyObject* const* a, Py_ssize_t n) {
+    count_args(n, 10);
+    filled_here(a[9], "cache");
+    const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
+    int32_t* table = contiguous<int32_t>(&required(a[1], "table"), {c.batch, c.max_pages}, at::kInt, "table");
+    const at::Tensor& refs = required(a[2], "refs");
+    int32_t* held = contiguous<int32_t>(&refs, {c.pages}, at::kInt, "refs");
+    const int32_t *length = each_sequence(a[3], c, "length"), *source = per_sequence(a[4], c, "source");
+    const int32_t* drop = contiguous<int32_t>(tensor(a[5], "drop"), {c.batch, 2}, at::kInt, "drop");
+    const int32_t* count = per_sequence(a[6], c, "count");
+    const bool given = a[7] != Py_None;
+    const at::Tensor room = given ? required(a[7], "room") : at::empty({c.batch}, refs.options());
+    int32_t* room_p = contiguous<int32_t>(&room, {c.batch}, at::kInt, "room");
+    size_t bytes = 0;
+    check("vsa2_cache_assign_workspace", vsa2_cache_assign_workspace(&c, &bytes));
+    const at::Tensor ws = at::empty({static_cast<int64_t>(bytes)}, refs.options().dtype(at::kByte));
+    const hipStream_t s = stream_of(a[8]);
+    check("vsa2_cache_assign",
+          vsa2_cache_assign(&c, table, held, length, source, drop, count, room_p, ws.data_ptr(), bytes, s));
+    if (!given) return wrap(room);
+    Py_INCREF(a[7]);
+    return a[7];
+}
+
+// (from, to, index, start, count, stream, both devices)
+PyObject* cache_copy(PyObject* const* a, Py_ssize_t n) {
+    count_args(n, 8);
+    filled_here(a[6], "src");
+    filled_here(a[7], "dst");
+    const vsa2_cache &from = *structure<vsa2_cache>(a[0], "src"), &to = *structure<vsa2_cache>(a[1], "dst");
+    const at::Tensor& index = required(a[2], "index");
+    if (index.dim() != 2 || index.size(1) > INT32_MAX) fail("index: expected [batch, n], got " + shape_text(index.sizes()));
+    const int32_t* at_ = contiguous<int32_t>(&index, {to.batch, index.size(1)}, at::kInt, "index");
+    const int32_t *start = each_sequence(a[3], to, "start"), *count = per_sequence(a[4], to, "count");
+    const hipStream_t s = stream_of(a[5]);
+    check("vsa2_cache_copy", vsa2_cache_copy(&from, &to, static_cast<int32_t>(index.size(1)), at_, start, count, s));
+    Py_RETURN_NONE;
 }
 
 PyObject* set_error(PyObject* const* a, Py_ssize_t n) {
@@ -441,6 +550,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define VSA2_ENTRY(F) {#F, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<F>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {VSA2_ENTRY(fill_rope),   VSA2_ENTRY(fill_cache), VSA2_ENTRY(norm_rope), VSA2_ENTRY(norm_rope_bwd),
                            VSA2_ENTRY(cache_write), VSA2_ENTRY(cache_read), VSA2_ENTRY(attn_cache), VSA2_ENTRY(set_error),
+                           VSA2_ENTRY(attn_cache_shared), VSA2_ENTRY(attn_cache_scored), VSA2_ENTRY(cache_assign),
+                           VSA2_ENTRY(cache_copy),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host", "Argument marshalling of the helpers around the attention.", -1,
                         g_methods, nullptr, nullptr, nullptr, nullptr};

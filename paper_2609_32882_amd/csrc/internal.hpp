@@ -232,4 +232,31 @@ hipError_t launch_attn_cache(int dtype, int D, const cache_view& c, int heads_q,
                              const int32_t* length, const int32_t* count, bool causal, const row_view& o, float* lse,
                              void* ws, hipStream_t s);
 
+// The same with changed scores and ranges of positions (attn_cache_scored.hip).
+struct score_options {
+    const float* slope;      // [heads_q] or null
+    const int32_t* span;     // [batch][n][2] or null
+    int window, sink;        // 0: none
+    float cap;               // 0: none
+};
+size_t attn_cache_scored_workspace_bytes(const cache_view& c, int D, int heads_q, int n, int window, int sink);
+hipError_t launch_attn_cache_scored(int dtype, int D, const cache_view& c, int heads_q, int n, const row_view& q,
+                                    const int32_t* length, const int32_t* count, bool causal, const score_options& options,
+                                    const row_view& o, float* lse, void* ws, hipStream_t s);
+// Attention over a list that several sequences share and their own ones (attn_cache_shared.hip):
+// sequence b of c reads list b / (c.batch / pre.batch) of pre first.
+size_t attn_cache_shared_workspace_bytes(const cache_view& pre, const cache_view& c, int D, int heads_q, int n);
+hipError_t launch_attn_cache_shared(int dtype, int D, const cache_view& pre, const cache_view& c, int heads_q, int n,
+                                    const row_view& q, const int32_t* pre_length, const int32_t* length,
+                                    const int32_t* count, bool causal, const row_view& o, float* lse, void* ws,
+                                    hipStream_t s);
+// The cache's page lists (cache_lists.hip).  table and refs are changed.
+size_t cache_assign_workspace_bytes(const cache_view& c);
+hipError_t launch_cache_assign(int D, const cache_view& c, int32_t* table, int32_t* refs, const int32_t* length,
+                               const int32_t* source, const int32_t* drop, const int32_t* count, int32_t* room,
+                               void* ws, hipStream_t s);
+// Tokens from one cache's lists to another's, as they are stored.
+hipError_t launch_cache_move(int D, const cache_view& from, const cache_view& to, int n, const int32_t* index,
+                             const int32_t* start, const int32_t* count, hipStream_t s);
+
 }  // namespace vsa2

@@ -1,12 +1,13 @@
 // The page lists of the paged 8-bit cache: which pages every sequence's list holds,
 // how often a page is held, and copies of tokens between lists.
 //
-// Assigning lists is index work, bound by the latency of launches and of steps that wait
-// for one another, unless pages are copied.  Where lists move, one launch saves the old
-// lists and gives up their pages, a second writes the new ones; a single workgroup then
-// settles who copies a shared last page, numbers the requests for pages in order of the
-// sequences, and hands out the free pages in order of their index; the last launch copies
-// pages.  Counts are changed with whole-number atomics, whose order is of no
+// Assigning lists is index work, bound by the latency of launches and of loads that wait
+// for one another, unless pages are copied.  One workgroup does it where the lists fit its
+// LDS: it saves the old lists, gives up their pages, writes the new lists, settles who
+// copies a shared last page, numbers the requests for pages in order of the sequences, and
+// hands out the free pages in order of their index; a second launch copies pages.  Longer
+// lists are moved by launches of their own, larger pools searched by a workgroup for every
+// 16,384 pages.  Counts are changed with whole-number atomics, whose order is of no
 // consequence; every choice goes by indices.
 #include <algorithm>
 
@@ -20,15 +21,15 @@ constexpr int NT = 1024;                 // threads of the planning workgroup
 constexpr int PER = 16;                  // pages a thread looks at in a step
 constexpr int STEP = NT * PER;           // pages of a step
 constexpr int LONE_STEPS = 4;            // steps that one workgroup takes alone
-constexpr int LONE_ENTRIES = 8192;       // list entries that it trims by itself
-constexpr int FINDERS = 4096;            // sequences whose request numbers it keeps in LDS
+constexpr int LONE_ENTRIES = 24576;      // list entries that it keeps in LDS
+constexpr int LONE_FORKS = 2048;         // and where sequences take others' lists
 
 enum last_page { NONE, KEEPS, COPIES, STUCK };      // what a sequence does about its shared last page
 
 // Per sequence: pages kept, requests before it, pages wanted behind the kept ones, last_page,
-// its page, the copy's page.
+// its page, the copy's page, places left in the kept pages, tokens to make room for.
 struct seq_info {
-    int kept, base, wanted, last, page, copy;
+    int kept, base, wanted, last, page, copy, slack, count;
 };
 
 struct assign_args {
@@ -40,8 +41,7 @@ struct assign_args {
     int32_t* old;            // [batch][max_pages]
     seq_info* info;          // [batch]
     int32_t* free_pages;     // of each step
-    int32_t* totals;         // requests, free pages
-    bool trims, lone;        // the planning workgroup trims the lists; it hands out the pages
+    int32_t* totals;         // requests
 };
 
 __device__ __forceinline__ bool is_page(const assign_args& a, int e) { return e >= 0 && e < a.c.pages; }
@@ -56,47 +56,77 @@ __device__ __forceinline__ int64_t kept_tokens(const assign_args& a, int b) {
 }
 __device__ __forceinline__ int pages_of(int64_t tokens) { return static_cast<int>((tokens + CACHE_TOKENS - 1) / CACHE_TOKENS); }
 
-// Where entry s of sequence b's new list comes from, -1 for nowhere.
-struct entry_source {
-    int src, at;
-    bool stays;          // the same place of the same list
+// What becomes of a sequence's list.
+struct list_move {
+    int kept, src, first, num;
+    // where new entry s comes from, -1 for nowhere
+    __device__ __forceinline__ int from(int s, int max_pages) const {
+        const int64_t at = s + (s >= first ? static_cast<int64_t>(num) : 0);
+        return s < kept && at < max_pages ? static_cast<int>(at) : -1;
+    }
+    // does old entry s stay in the list (at any place)?
+    __device__ __forceinline__ bool retains(int b, int s) const {
+        if (src != b) return false;
+        return s < first ? s < kept : s - static_cast<int64_t>(first) >= num && s - static_cast<int64_t>(num) < kept;
+    }
 };
-__device__ __forceinline__ entry_source entry_of(const assign_args& a, int b, int s) {
-    if (s >= pages_of(kept_tokens(a, b))) return {0, -1, false};
-    const int src = source_of(a, b);
-    int64_t at = s;
-    if (a.drop && s >= a.drop[2 * b]) at += max(a.drop[2 * b + 1], 0);
-    return {src, at < a.c.max_pages ? static_cast<int>(at) : -1, src == b && at == s};
+__device__ __forceinline__ list_move move_of(const assign_args& a, int b) {
+    list_move w{pages_of(kept_tokens(a, b)), source_of(a, b), 0, 0};
+    if (a.drop) {
+        w.first = max(a.drop[2 * b], 0);
+        w.num = max(a.drop[2 * b + 1], 0);
+    }
+    return w;
 }
 
 __device__ __forceinline__ int held(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// The old lists are saved and, where an entry does not stay, its page is given up.
+// The old lists are saved, and the pages that leave them given up.
 __global__ __launch_bounds__(256) void lists_save_kernel(assign_args a) {
     const int64_t all = static_cast<int64_t>(a.c.batch) * a.c.max_pages;
     for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < all; x += static_cast<int64_t>(gridDim.x) * 256) {
         const int b = static_cast<int>(x / a.c.max_pages), s = static_cast<int>(x - static_cast<int64_t>(b) * a.c.max_pages);
         const int e = a.table[x];
         a.old[x] = e;
-        if (is_page(a, e) && !entry_of(a, b, s).stays) atomicAdd(a.refs + e, -1);
+        if (is_page(a, e) && !move_of(a, b).retains(b, s)) atomicAdd(a.refs + e, -1);
     }
 }
 __global__ __launch_bounds__(256) void lists_write_kernel(assign_args a) {
     const int64_t all = static_cast<int64_t>(a.c.batch) * a.c.max_pages;
     for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < all; x += static_cast<int64_t>(gridDim.x) * 256) {
         const int b = static_cast<int>(x / a.c.max_pages), s = static_cast<int>(x - static_cast<int64_t>(b) * a.c.max_pages);
-        const entry_source from = entry_of(a, b, s);
-        int e = from.at < 0 ? -1 : a.old[static_cast<int64_t>(from.src) * a.c.max_pages + from.at];
+        const list_move w = move_of(a, b);
+        const int at = w.from(s, a.c.max_pages);
+        int e = at < 0 ? -1 : a.old[static_cast<int64_t>(w.src) * a.c.max_pages + at];
         if (!is_page(a, e)) e = -1;
         a.table[x] = e;
-        if (e >= 0 && !from.stays) atomicAdd(a.refs + e, 1);
+        if (e >= 0 && w.src != b) atomicAdd(a.refs + e, 1);
+    }
+}
+
+// Lists that go on from others' without losing pages: entries stay in their columns, so a workgroup
+// that holds some columns of all lists saves and writes them in one launch.
+constexpr int COLUMN_ENTRIES = 8192;
+__global__ __launch_bounds__(256) void lists_columns_kernel(assign_args a, int columns) {
+    __shared__ int old[COLUMN_ENTRIES];
+    const int s0 = blockIdx.x * columns, n = min(columns, a.c.max_pages - s0), all = a.c.batch * n;
+    for (int x = threadIdx.x; x < all; x += 256) old[x] = a.table[static_cast<int64_t>(x / n) * a.c.max_pages + s0 + x % n];
+    __syncthreads();
+    for (int x = threadIdx.x; x < all; x += 256) {
+        const int b = x / n, i = x - b * n, s = s0 + i, was = old[x];
+        const list_move w = move_of(a, b);
+        int e = s < w.kept ? old[w.src * n + i] : -1;
+        if (!is_page(a, e)) e = -1;
+        if (is_page(a, was) && !w.retains(b, s)) atomicAdd(a.refs + was, -1);
+        if (e >= 0 && w.src != b) atomicAdd(a.refs + e, 1);
+        if (e != was) a.table[static_cast<int64_t>(b) * a.c.max_pages + s] = e;
     }
 }
 
 // Lists that all stay: pages behind the kept ones are given up.
-__device__ __forceinline__ void trim(const assign_args& a, int64_t first, int64_t step) {
+__global__ __launch_bounds__(256) void lists_trim_kernel(assign_args a) {
     const int64_t all = static_cast<int64_t>(a.c.batch) * a.c.max_pages;
-    for (int64_t x = first; x < all; x += step) {
+    for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < all; x += static_cast<int64_t>(gridDim.x) * 256) {
         const int b = static_cast<int>(x / a.c.max_pages), s = static_cast<int>(x - static_cast<int64_t>(b) * a.c.max_pages);
         const int e = a.table[x];
         const bool page = is_page(a, e);
@@ -108,187 +138,280 @@ __device__ __forceinline__ void trim(const assign_args& a, int64_t first, int64_
         if (e != -1) a.table[x] = -1;
     }
 }
-__global__ __launch_bounds__(256) void lists_trim_kernel(assign_args a) {
-    trim(a, static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, static_cast<int64_t>(gridDim.x) * 256);
+
+// Inclusive sum over a wave's lanes up to each lane.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // rows of 16 lanes: 1, 2, 4, 8 back
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // a row's last lane to the next row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // the first half's to the second
+    return x;
 }
 
-// Exclusive prefix over the workgroup's threads, and the total.
-__device__ __forceinline__ int prefix(int x, int* sums, int& total) {
-    const int lane = lane_id(), wave = wave_id();
-    int y = x;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-        const int z = __shfl_up(y, k, 64);
-        if (lane >= k) y += z;
-    }
-    if (lane == 63) sums[wave] = y;
+// Exclusive prefix over the workgroup's threads, and the total.  One barrier: calls that follow each
+// other take turns with two arrays of sums.
+struct wg_sums {
+    int of[2][NT / 64];
+};
+__device__ __forceinline__ int prefix(int x, wg_sums& sums, int turn, int& total) {
+    const int y = wave_prefix(x);
+    int (&mine)[NT / 64] = sums.of[turn & 1];
+    if (lane_id() == 63) mine[wave_id()] = y;
     __syncthreads();
     int before = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-        before += w < wave ? sums[w] : 0;
-        total += sums[w];
+        const int z = mine[w];
+        before += w < wave_id() ? z : 0;
+        total += z;
     }
-    __syncthreads();
     return before + y - x;
 }
 
-// Who copies its last page, and every sequence's first request.  A sequence that writes into
-// a kept page takes itself off the page's count; where nobody else is left, the last of
-// them (by index) keeps it, the others need copies.
-__device__ void plan_requests(const assign_args& a, int* sums, int* bases) {
-    const int tid = threadIdx.x, batch = a.c.batch;
-    for (int b = tid; b < batch; b += NT) {
-        const int64_t n = kept_tokens(a, b), count = a.count ? max(a.count[b], 0) : 0;
-        seq_info w{pages_of(n), 0, 0, NONE, -1, -1};
-        const int64_t end = (n + count + CACHE_TOKENS - 1) / CACHE_TOKENS;
-        w.wanted = static_cast<int>(min(end, static_cast<int64_t>(a.c.max_pages))) - w.kept;
-        if (count > 0 && n % CACHE_TOKENS) {
-            w.page = a.table[static_cast<int64_t>(b) * a.c.max_pages + w.kept - 1];
-            w.last = w.page < 0 ? STUCK : KEEPS;
-            if (w.page >= 0) atomicAdd(a.refs + w.page, -1);
-        }
-        a.info[b] = w;
-    }
-    __syncthreads();
-    for (int b = tid; b < batch; b += NT)
-        if (a.info[b].last == KEEPS && held(a.refs + a.info[b].page) <= 0) atomicMin(a.refs + a.info[b].page, -(b + 1));
-    __syncthreads();
-    for (int b = tid; b < batch; b += NT)
-        if (a.info[b].last == KEEPS && held(a.refs + a.info[b].page) != -(b + 1)) a.info[b].last = COPIES;
-    __syncthreads();
-    int all = 0;
-    for (int b0 = 0; b0 < batch; b0 += NT) {
-        const int b = b0 + tid;
-        int need = 0;
-        if (b < batch) {
-            if (a.info[b].last == KEEPS) __hip_atomic_store(a.refs + a.info[b].page, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            need = a.info[b].wanted + (a.info[b].last == COPIES ? 1 : 0);
-        }
-        int total;
-        const int base = all + prefix(need, sums, total);
-        if (b < batch) {
-            a.info[b].base = base;
-            if (batch <= FINDERS) bases[b] = base;
-        }
-        all += total;
-    }
-    if (tid == 0) a.totals[0] = all;
-    __syncthreads();
-    __threadfence();         // the counts below are read past what this CU may hold of them
+// A sequence before its requests are numbered; its last page follows where it writes into one
+// (`inside`).
+__device__ __forceinline__ seq_info info_of(const assign_args& a, int b, bool& inside) {
+    const int count = a.count ? max(a.count[b], 0) : 0;
+    const int64_t n = kept_tokens(a, b), end = (n + count + CACHE_TOKENS - 1) / CACHE_TOKENS;
+    seq_info w{pages_of(n), 0, 0, NONE, -1, -1, static_cast<int>(-n & (CACHE_TOKENS - 1)), count};
+    w.wanted = static_cast<int>(min(end, static_cast<int64_t>(a.c.max_pages))) - w.kept;
+    inside = count > 0 && w.slack > 0;
+    if (inside) w.last = STUCK;
+    return w;
 }
 
-// Sixteen counts from page p0 on: a bit for each free page.
-__device__ __forceinline__ uint32_t free_bits(const assign_args& a, int64_t p0) {
-    uint32_t bits = 0;
+// Who copies its last page, and every sequence's first request; returns all requests.  A sequence
+// that writes into a kept page which others hold, too, takes itself off the page's count; where
+// nobody else is left, the last of them (by index) keeps it, the others need copies.  No count
+// becomes 0 or stops being 0 here.
+__device__ __forceinline__ int plan_requests(const assign_args& a, seq_info* info, wg_sums& sums) {
+    const int tid = threadIdx.x, batch = a.c.batch;
+    bool shared = false;
+    for (int b = tid; b < batch; b += NT) {
+        const int page = info[b].page;
+        if (page < 0) continue;
+        const bool copies = held(a.refs + page) != 1;
+        info[b].last = copies ? COPIES : KEEPS;
+        shared |= copies;
+    }
+    if (__syncthreads_or(shared)) {
+        for (int b = tid; b < batch; b += NT)
+            if (info[b].last == COPIES) atomicAdd(a.refs + info[b].page, -1);
+        __syncthreads();
+        for (int b = tid; b < batch; b += NT)
+            if (info[b].last == COPIES && held(a.refs + info[b].page) <= 0) atomicMin(a.refs + info[b].page, -(b + 1));
+        __syncthreads();
+        for (int b = tid; b < batch; b += NT)
+            if (info[b].last == COPIES && held(a.refs + info[b].page) == -(b + 1)) info[b].last = KEEPS;
+        __syncthreads();
+        for (int b = tid; b < batch; b += NT)
+            if (info[b].last == KEEPS) __hip_atomic_store(a.refs + info[b].page, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    int all = 0;
+    for (int b0 = 0, turn = 0; b0 < batch; b0 += NT, ++turn) {
+        const int b = b0 + tid;
+        const int need = b < batch ? info[b].wanted + (info[b].last == COPIES ? 1 : 0) : 0;
+        int total;
+        const int base = all + prefix(need, sums, turn, total);
+        if (b < batch) info[b].base = base;
+        all += total;
+    }
+    __syncthreads();         // the sums are free again
+    return all;
+}
+
+// Sixteen counts from page p0 on, read past what this CU may hold of them; those past the
+// pool as 1.
+struct counts16 {
+    uint64_t two[PER / 2];
+};
+__device__ __forceinline__ counts16 load_counts(const assign_args& a, int64_t p0) {
+    counts16 c;
     if (p0 + PER <= a.c.pages) {
 #pragma unroll
-        for (int i = 0; i < PER; i += 4) {
-            const int4 r = *reinterpret_cast<const int4*>(a.refs + p0 + i);
-            bits |= (r.x == 0 ? 1u : 0u) << i | (r.y == 0 ? 2u : 0u) << i | (r.z == 0 ? 4u : 0u) << i | (r.w == 0 ? 8u : 0u) << i;
-        }
-    } else {
-        for (int i = 0; i < PER; ++i)
-            if (p0 + i < a.c.pages && a.refs[p0 + i] == 0) bits |= 1u << i;
+        for (int i = 0; i < PER / 2; ++i)
+            c.two[i] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(a.refs + p0) + i, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+        return c;
     }
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i) {
+        c.two[i] = 0x0000000100000001ull;
+        if (p0 + 2 * i + 1 < a.c.pages)
+            c.two[i] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(a.refs + p0) + i, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+        else if (p0 + 2 * i < a.c.pages)
+            c.two[i] = static_cast<uint32_t>(held(a.refs + p0 + 2 * i)) | 0x0000000100000000ull;
+    }
+    return c;
+}
+// A bit for each free page.
+__device__ __forceinline__ uint32_t free_bits(const counts16& c) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i)
+        bits |= (static_cast<uint32_t>(c.two[i]) == 0 ? 1u : 0u) << (2 * i) | ((c.two[i] >> 32) == 0 ? 2u : 0u) << (2 * i);
     return bits;
 }
 
-// Hands the free pages of `bits`, the first of which is number `rank`, to the requests.
-__device__ __forceinline__ void hand_out(const assign_args& a, int64_t p0, uint32_t bits, int64_t rank, int requests,
-                                         const int* bases) {
-    for (; bits && rank < requests; ++rank) {
-        const int i = __builtin_ctz(bits);
-        bits &= bits - 1;
-        const int page = static_cast<int>(p0 + i);
-        int lo = 0, hi = a.c.batch - 1;           // the last sequence whose first request is not past it
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if ((bases ? bases[mid] : a.info[mid].base) <= rank) lo = mid;
-            else hi = mid - 1;
-        }
-        const seq_info w = a.info[lo];
-        const int nth = static_cast<int>(rank) - w.base - (w.last == COPIES ? 1 : 0);
-        if (nth < 0) a.info[lo].copy = page;
-        else a.table[static_cast<int64_t>(lo) * a.c.max_pages + w.kept + nth] = page;
-        a.refs[page] = 1;
+// Gives a page to request number `rank`.
+__device__ __forceinline__ void give(const assign_args& a, seq_info* info, int rank, int page) {
+    int lo = 0, hi = a.c.batch - 1;           // the last sequence whose first request is not past it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (info[mid].base <= rank) lo = mid;
+        else hi = mid - 1;
     }
+    const seq_info w = info[lo];
+    const int nth = rank - w.base - (w.last == COPIES ? 1 : 0);
+    if (nth < 0) info[lo].copy = page;
+    else a.table[static_cast<int64_t>(lo) * a.c.max_pages + w.kept + nth] = page;
+    a.refs[page] = 1;
+}
+
+// Gives the free pages of a step, `before` of which come before it, to the requests; list: LDS for
+// the step's free pages, so that every thread has a request.
+__device__ __forceinline__ int give_step(const assign_args& a, seq_info* info, const counts16& counts, int64_t p0,
+                                         int64_t before, int requests, wg_sums& sums, int* list) {
+    const int64_t mine = p0 + threadIdx.x * PER;
+    uint32_t bits = free_bits(counts);
+    int total;
+    int at = prefix(__popc(bits), sums, 0, total);
+    for (; bits && before + at < requests; ++at) {
+        list[at] = static_cast<int>(mine + __builtin_ctz(bits));
+        bits &= bits - 1;
+    }
+    __syncthreads();
+    const int64_t left = requests - before;
+    for (int i = threadIdx.x; i < total && i < left; i += NT) give(a, info, static_cast<int>(before + i), list[i]);
+    __syncthreads();
+    return total;
 }
 
 // What the requests got.  Sequences whose copy was refused are holders of the page again, and then
 // nobody may write into it.
-__device__ void finish(const assign_args& a, int64_t found) {
+__device__ __forceinline__ void finish(const assign_args& a, seq_info* info, int64_t found, int requests) {
     const int tid = threadIdx.x, batch = a.c.batch;
+    bool refused = false;
     for (int b = tid; b < batch; b += NT) {
-        const seq_info w = a.info[b];
+        const seq_info w = info[b];
         if (w.last != COPIES) continue;
-        if (w.base < found) a.table[static_cast<int64_t>(b) * a.c.max_pages + w.kept - 1] = w.copy;
-        else atomicAdd(a.refs + w.page, 1);
+        if (w.base < found) {
+            a.table[static_cast<int64_t>(b) * a.c.max_pages + w.kept - 1] = w.copy;
+        } else {
+            atomicAdd(a.refs + w.page, 1);
+            refused = true;
+        }
     }
-    __syncthreads();
+    if (found < requests) refused = __syncthreads_or(refused);
     for (int b = tid; a.room && b < batch; b += NT) {
-        const seq_info w = a.info[b];
-        const int64_t count = a.count ? max(a.count[b], 0) : 0, n = kept_tokens(a, b);
+        const seq_info w = info[b];
         const int copies = w.last == COPIES ? 1 : 0;
         const int64_t left = found - w.base - copies;
-        const int64_t got = left < 0 ? 0 : (left < w.wanted ? left : w.wanted);
-        int64_t room = (w.kept + got) * CACHE_TOKENS - n;
-        room = room < count ? room : count;
-        const bool alone = w.last == NONE || (w.last == KEEPS && held(a.refs + w.page) <= 1) || (copies && w.base < found);
-        a.room[b] = alone && room > 0 ? static_cast<int>(room) : 0;
+        const int got = static_cast<int>(left < 0 ? 0 : (left < w.wanted ? left : w.wanted));
+        const int room = min(got * CACHE_TOKENS + w.slack, w.count);
+        const bool alone = w.last == NONE || (copies && w.base < found) ||
+                           (w.last == KEEPS && (!refused || held(a.refs + w.page) <= 1));
+        a.room[b] = alone ? room : 0;
     }
 }
 
-__global__ __launch_bounds__(NT) void lists_plan_kernel(assign_args a) {
-    __shared__ int sums[NT / 64], bases[FINDERS];
-    if (a.trims) {
-        trim(a, threadIdx.x, NT);
-        __syncthreads();
-    }
-    plan_requests(a, sums, bases);
-    if (!a.lone) return;
-    const int requests = a.totals[0];
-    int found = 0;
-    for (int64_t p0 = 0; p0 < a.c.pages && found < requests; p0 += STEP) {
-        const int64_t mine = p0 + threadIdx.x * PER;
-        const uint32_t bits = free_bits(a, mine);
-        int total;
-        const int rank = found + prefix(__popc(bits), sums, total);
-        hand_out(a, mine, bits, rank, requests, a.c.batch <= FINDERS ? bases : nullptr);
-        found += total;
+// Up to NT sequences whose lists fit LDS, in a pool of LONE_STEPS steps: all but the copies.
+__global__ __launch_bounds__(NT) void lists_alone_kernel(assign_args a) {
+    __shared__ seq_info info[NT];
+    __shared__ list_move moves[NT];
+    __shared__ wg_sums sums;
+    __shared__ int old[LONE_ENTRIES];
+    static_assert(LONE_ENTRIES >= STEP, "the free pages of a step go there, too");
+    const int tid = threadIdx.x, m = a.c.max_pages, all = a.c.batch * m;
+    const float per = 1.f / static_cast<float>(m);
+    bool inside = false;
+    for (int x = tid; x < all; x += NT) old[x] = a.table[x];
+    if (tid < a.c.batch) {
+        moves[tid] = move_of(a, tid);
+        info[tid] = info_of(a, tid, inside);
     }
     __syncthreads();
-    finish(a, found);
+    for (int x = tid; x < all; x += NT) {
+        // x / m, off by at most 2^-22 of it: less than the half that is added is from a whole number
+        const int b = static_cast<int>((static_cast<float>(x) + 0.5f) * per), s = x - b * m, was = old[x];
+        const list_move w = moves[b];
+        const int at = w.from(s, m);
+        int e = at < 0 ? -1 : old[w.src * m + at];
+        if (!is_page(a, e)) e = -1;
+        if (is_page(a, was) && !w.retains(b, s)) atomicAdd(a.refs + was, -1);
+        if (e >= 0 && w.src != b) atomicAdd(a.refs + e, 1);
+        if (e != was) a.table[x] = e;
+        if (s == w.kept - 1 && info[b].last == STUCK) info[b].page = e;
+    }
+    __syncthreads();
+    counts16 counts = load_counts(a, tid * PER);        // under way while the requests are numbered
+    const int requests = plan_requests(a, info, sums);
+    int64_t found = 0;
+    for (int64_t p0 = 0; p0 < a.c.pages && found < requests; p0 += STEP) {
+        if (p0) counts = load_counts(a, p0 + tid * PER);
+        found += give_step(a, info, counts, p0, found, requests, sums, old);
+    }
+    finish(a, info, found, requests);
+    if (tid < a.c.batch) a.info[tid] = info[tid];
+}
+
+// Lists that other launches have moved: the pages, all of them (LONE) or in launches that follow.
+template <bool LONE, bool FEW>
+__global__ __launch_bounds__(NT) void lists_plan_kernel(assign_args a) {
+    __shared__ seq_info own[FEW ? NT : 1];
+    __shared__ wg_sums sums;
+    __shared__ int list[LONE ? STEP : 1];
+    seq_info* info = FEW ? own : a.info;
+    counts16 counts = LONE ? load_counts(a, threadIdx.x * PER) : counts16{};
+    for (int b = threadIdx.x; b < a.c.batch; b += NT) {
+        bool inside;
+        seq_info w = info_of(a, b, inside);
+        if (inside) w.page = a.table[static_cast<int64_t>(b) * a.c.max_pages + w.kept - 1];
+        info[b] = w;
+    }
+    const int requests = plan_requests(a, info, sums);
+    if constexpr (LONE) {
+        int64_t found = 0;
+        for (int64_t p0 = 0; p0 < a.c.pages && found < requests; p0 += STEP) {
+            if (p0) counts = load_counts(a, p0 + threadIdx.x * PER);
+            found += give_step(a, info, counts, p0, found, requests, sums, list);
+        }
+        finish(a, info, found, requests);
+        for (int b = threadIdx.x; FEW && b < a.c.batch; b += NT) a.info[b] = info[b];
+    } else {
+        if (threadIdx.x == 0) a.totals[0] = requests;
+    }
 }
 
 // Large pools: a workgroup for every step, which counts its free pages first.
 __global__ __launch_bounds__(NT) void lists_count_kernel(assign_args a) {
-    __shared__ int sums[NT / 64];
+    __shared__ wg_sums sums;
     int total;
-    prefix(__popc(free_bits(a, static_cast<int64_t>(blockIdx.x) * STEP + threadIdx.x * PER)), sums, total);
+    prefix(__popc(free_bits(load_counts(a, static_cast<int64_t>(blockIdx.x) * STEP + threadIdx.x * PER))), sums, 0, total);
     if (threadIdx.x == 0) a.free_pages[blockIdx.x] = total;
 }
-__device__ __forceinline__ int64_t free_before(const assign_args& a, int steps, int* sums) {
+__device__ __forceinline__ int64_t free_before(const assign_args& a, int steps, wg_sums& sums) {
     int mine = 0, total;             // pages are 31 bits, so is their sum
     for (int i = threadIdx.x; i < steps; i += NT) mine += a.free_pages[i];
-    prefix(mine, sums, total);
+    prefix(mine, sums, 1, total);
     return total;
 }
-__global__ __launch_bounds__(NT) void lists_hand_kernel(assign_args a) {
-    __shared__ int sums[NT / 64];
+__global__ __launch_bounds__(NT) void lists_give_kernel(assign_args a) {
+    __shared__ wg_sums sums;
+    __shared__ int list[STEP];
     const int64_t before = free_before(a, blockIdx.x, sums);
     const int requests = a.totals[0];
     if (before >= requests) return;
-    const int64_t mine = static_cast<int64_t>(blockIdx.x) * STEP + threadIdx.x * PER;
-    const uint32_t bits = free_bits(a, mine);
-    int total;
-    const int64_t rank = before + prefix(__popc(bits), sums, total);
-    hand_out(a, mine, bits, rank, requests, nullptr);
+    const int64_t p0 = static_cast<int64_t>(blockIdx.x) * STEP;
+    give_step(a, a.info, load_counts(a, p0 + threadIdx.x * PER), p0, before, requests, sums, list);
 }
 __global__ __launch_bounds__(NT) void lists_finish_kernel(assign_args a, int steps) {
-    __shared__ int sums[NT / 64];
-    finish(a, free_before(a, steps, sums));
+    __shared__ wg_sums sums;
+    finish(a, a.info, free_before(a, steps, sums), a.totals[0]);
 }
 
 // Pages that got a copy: 16 KB a workgroup.
@@ -424,21 +547,31 @@ hipError_t launch_cache_assign(int D, const cache_view& c, int32_t* table, int32
     w += up256(static_cast<size_t>(steps_of(c.pages)) * sizeof(int32_t));
     a.totals = reinterpret_cast<int32_t*>(w);
     const int64_t entries = static_cast<int64_t>(c.batch) * c.max_pages, steps = steps_of(c.pages);
-    const dim3 wide(static_cast<unsigned>(std::min<int64_t>((entries + 255) / 256, 4096)));
-    a.lone = steps <= LONE_STEPS;
-    if (source || drop) {
-        hipLaunchKernelGGL(lists_save_kernel, wide, dim3(256), 0, s, a);
-        hipLaunchKernelGGL(lists_write_kernel, wide, dim3(256), 0, s, a);
-    } else if (entries <= LONE_ENTRIES) {
-        a.trims = true;
+    if (c.batch <= NT && entries <= (source ? LONE_FORKS : LONE_ENTRIES) && steps <= LONE_STEPS) {
+        hipLaunchKernelGGL(lists_alone_kernel, dim3(1), dim3(NT), 0, s, a);
     } else {
-        hipLaunchKernelGGL(lists_trim_kernel, wide, dim3(256), 0, s, a);
-    }
-    hipLaunchKernelGGL(lists_plan_kernel, dim3(1), dim3(NT), 0, s, a);
-    if (!a.lone) {
-        hipLaunchKernelGGL(lists_count_kernel, dim3(static_cast<unsigned>(steps)), dim3(NT), 0, s, a);
-        hipLaunchKernelGGL(lists_hand_kernel, dim3(static_cast<unsigned>(steps)), dim3(NT), 0, s, a);
-        hipLaunchKernelGGL(lists_finish_kernel, dim3(1), dim3(NT), 0, s, a, static_cast<int>(steps));
+        const dim3 wide(static_cast<unsigned>(std::min<int64_t>((entries + 255) / 256, 4096)));
+        if (source && !drop && c.batch * 4 <= COLUMN_ENTRIES) {
+            // at least a column for every two of the 256 CUs
+            const int columns = static_cast<int>(std::max<int64_t>(
+                1, std::min<int64_t>(COLUMN_ENTRIES / c.batch, (c.max_pages + 511) / 512)));
+            hipLaunchKernelGGL(lists_columns_kernel, dim3(static_cast<unsigned>((c.max_pages + columns - 1) / columns)), dim3(256),
+                               0, s, a, columns);
+        } else if (source || drop) {
+            hipLaunchKernelGGL(lists_save_kernel, wide, dim3(256), 0, s, a);
+            hipLaunchKernelGGL(lists_write_kernel, wide, dim3(256), 0, s, a);
+        } else {
+            hipLaunchKernelGGL(lists_trim_kernel, wide, dim3(256), 0, s, a);
+        }
+        if (steps <= LONE_STEPS) {
+            if (c.batch <= NT) hipLaunchKernelGGL((lists_plan_kernel<true, true>), dim3(1), dim3(NT), 0, s, a);
+            else hipLaunchKernelGGL((lists_plan_kernel<true, false>), dim3(1), dim3(NT), 0, s, a);
+        } else {
+            hipLaunchKernelGGL((lists_plan_kernel<false, false>), dim3(1), dim3(NT), 0, s, a);
+            hipLaunchKernelGGL(lists_count_kernel, dim3(static_cast<unsigned>(steps)), dim3(NT), 0, s, a);
+            hipLaunchKernelGGL(lists_give_kernel, dim3(static_cast<unsigned>(steps)), dim3(NT), 0, s, a);
+            hipLaunchKernelGGL(lists_finish_kernel, dim3(1), dim3(NT), 0, s, a, static_cast<int>(steps));
+        }
     }
     if (count) {
         const int64_t bytes = c.heads * cache_page_bytes(D);

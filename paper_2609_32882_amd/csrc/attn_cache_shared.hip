@@ -130,6 +130,40 @@ __global__ __launch_bounds__(SLICES > 8 ? 32 * SLICES : 256) void shared_join_ke
     if (lane == 0) store_lse(own, b, h, rr, base, l);
 }
 
+// What a workgroup's piece of `pages` takes, in us: a start and an end, then its pages, which
+// tiles' waves share out and rows' waves walk together.  Measured with two workgroups a CU (one
+// alone is faster by a third): 35,840 shared tokens, 8 heads of 128, 160 rows in pieces for 160
+// to 1,000 workgroups 45 to 67 us, this with 18 us around it within 4 of them.
+double piece_time(const side_plan& p, int dtype, int64_t pages, bool pairs) {
+    const int64_t n = (pages + p.splits - 1) / p.splits;
+    const double page = p.tile_rows == ROWS ? 2.4 : (pairs ? 2. : 1.5);
+    return 3. + (p.tile_rows == ROWS ? n : (n + 3) / 4) * (dtype == 0 ? 2. * page : page);
+}
+
+// Both sides' pieces on the 512 slots of two workgroups a CU, the shared ones first: when the last one
+// ends, and the partial results' way to memory and back.
+double call_time(const shared_plan& p, int dtype, int D, const int64_t (&pages)[2], const int64_t (&rows)[2], bool pairs) {
+    constexpr double SLOTS = 512.;
+    const double pre = piece_time(p.pre, dtype, pages[0], pairs), own = piece_time(p.own, dtype, pages[1], false);
+    const double n = static_cast<double>(p.pre.items()) * p.pre.splits;
+    double left = static_cast<double>(p.own.items()) * p.own.splits;
+    // slots by when they are free: `later` of them a piece after the others
+    const double rounds = static_cast<double>(static_cast<int64_t>(n / SLOTS)), later = n - rounds * SLOTS;
+    double early = rounds * pre, late = later > 0 ? early + pre : early;
+    const double step = left > 8 * SLOTS ? static_cast<double>(static_cast<int64_t>(left / SLOTS / 4)) : 1.;
+    while (left > 0) {
+        if (early <= late || later == 0) {
+            left -= (SLOTS - later) * step;
+            early += own * step;
+        } else {
+            left -= later * step;
+            late += own * step;
+        }
+    }
+    const double bytes = 8. * (D + 2) * rows[1] * p.own.lists * (p.pre.splits + p.own.splits);
+    return std::max(early, later > 0 ? late : early) + bytes / 4e6;
+}
+
 shared_plan plan_shared(int dtype, int D, const cache_view& pre, const cache_view& c, int heads_q, int n) {
     shared_plan p;
     const int64_t own_rows = static_cast<int64_t>(heads_q / c.heads) * n, pre_rows = own_rows * (c.batch / pre.batch);
@@ -140,18 +174,30 @@ shared_plan plan_shared(int dtype, int D, const cache_view& pre, const cache_vie
     p.pre.tile_rows = own_rows > 64 || pre_rows > 256 ? ROWS : (pairs ? 2 * TILE : TILE);
     const int64_t rows[2] = {pre_rows, own_rows}, pages[2] = {pre.max_pages, c.max_pages};
     side_plan* side[2] = {&p.pre, &p.own};
-    double cost[2], all = 0.;
+    int64_t most[2];
     for (int x = 0; x < 2; ++x) {
         side[x]->tiles = (rows[x] + side[x]->tile_rows - 1) / side[x]->tile_rows;
-        cost[x] = side[x]->tile_rows == ROWS ? 2. : x == 0 ? 0.5 : 1.;       // of a page
-        all += cost[x] * pages[x] * side[x]->items();
+        side[x]->splits = 1;
+        const int per = side[x]->tile_rows == ROWS ? 8 : 4;          // pages a piece has at least
+        most[x] = std::max<int64_t>(1, std::min<int64_t>((pages[x] + per - 1) / per, 1024 / side[x]->items()));
     }
-    for (int x = 0; x < 2; ++x) {
-        const int64_t most = (pages[x] + (side[x]->tile_rows == ROWS ? 7 : 3)) / (side[x]->tile_rows == ROWS ? 8 : 4);
-        const int64_t want = static_cast<int64_t>(cost[x] * pages[x] / (all / 1024.) + 0.5);
-        side[x]->splits = static_cast<int>(std::max<int64_t>(1, std::min(want, most)));
+    // the shared list for whole and half rounds of the slots, with and beside the own pieces
+    shared_plan best = p;
+    double least = -1.;
+    for (int64_t s = 1; s <= most[1]; s *= 2) {
+        for (int half = 1; half <= 4; ++half)
+            for (int beside = 0; beside < 2; ++beside) {
+                const int64_t room = 256 * half - beside * p.own.items() * s;
+                p.own.splits = static_cast<int>(s);
+                p.pre.splits = static_cast<int>(std::max<int64_t>(1, std::min(most[0], room / p.pre.items())));
+                const double t = call_time(p, dtype, D, pages, rows, pairs);
+                if (least < 0. || t < least) {
+                    least = t;
+                    best = p;
+                }
+            }
     }
-    return p;
+    return best;
 }
 
 // The pieces of either side spread over the XCDs as plan_args has it.

@@ -532,31 +532,34 @@ struct page_data {
     uint32_t ke;
 };
 template <int D>
-__device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
+__device__ __forceinline__ void load_keys(page_data<D>& pd, const char* page) {
     const int lane = lane_id();
     const uint4* kp = reinterpret_cast<const uint4*>(page) + lane;
-    const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
 #pragma unroll
     for (int i = 0; i < 4 * (D / 64); ++i) pd.k[i] = kp[i * 64];
     pd.ke = *reinterpret_cast<const uint32_t*>(page + 128 * D + (lane & 15) * 4);
+}
+template <int D>
+__device__ __forceinline__ void load_values(page_data<D>& pd, const char* page) {
+    const int lane = lane_id();
+    const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
     pd.ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + (lane >> 4) * 16);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) pd.v[i] = vp[i * 64];
+}
+template <int D>
+__device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
+    load_keys<D>(pd, page);
+    load_values<D>(pd, page);
     // all of them requested before the first is waited for
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// One page for XT tiles, decoded once for all of them.  MASKED: some row's limit,
-// or the list's end, may lie inside it.
-template <typename T, int D, int XT, bool MASKED, class SC>
-__device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos,
-                                          const typename SC::row (&row)[XT], int lim_max,
-                                          const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], const form_of_t<T, SC>& form,
-                                          tile_state<T, D> (&st)[XT], powers_seen& seen) {
+// S^T of one page for XT tiles, its keys decoded once for all of them.
+template <typename T, int D, int XT>
+__device__ __forceinline__ void page_scores(const page_data<D>& pd, const frag_bf16 (&qf)[XT][D / 32][terms_of<T>],
+                                            f32x4_t (&s)[XT][4]) {
     constexpr int NT = terms_of<T>;
-    const int g = lane_id() >> 4;
-    const float scale = SC::ON ? 1.f : form.scale;
-    f32x4_t s[XT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const float power = power_of((pd.ke >> (8 * t)) & 0xffu);
@@ -575,6 +578,17 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
                 }
         }
     }
+}
+
+// The rest of a page: softmax and the product with the values.  MASKED: some row's limit,
+// or the list's end, may lie inside it.
+template <typename T, int D, int XT, bool MASKED, class SC>
+__device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* page, int pos,
+                                           const typename SC::row (&row)[XT], int lim_max, f32x4_t (&s)[XT][4],
+                                           const form_of_t<T, SC>& form, tile_state<T, D> (&st)[XT], powers_seen& seen) {
+    constexpr int NT = terms_of<T>;
+    const int g = lane_id() >> 4;
+    const float scale = SC::ON ? 1.f : form.scale;
     uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
     uint4 vr[D / 16];
 #pragma unroll
@@ -754,6 +768,16 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
     }
 }
 
+template <typename T, int D, int XT, bool MASKED, class SC>
+__device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos,
+                                          const typename SC::row (&row)[XT], int lim_max,
+                                          const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], const form_of_t<T, SC>& form,
+                                          tile_state<T, D> (&st)[XT], powers_seen& seen) {
+    f32x4_t s[XT][4];
+    page_scores<T, D, XT>(pd, qf, s);
+    page_weigh<T, D, XT, MASKED, SC>(pd, page, pos, row, lim_max, s, form, st, seen);
+}
+
 // Element offset of row r (query head and token of KV head h) in q or o.
 template <rows_kind KIND = WHOLE>
 __device__ __forceinline__ int64_t row_offset(const row_view& v, const attn_args& a, int b, int h, int r) {
@@ -862,10 +886,27 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
     const auto page = [&]() { return a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D); };
     const auto whole = [&]() { return more && (SC::ON ? ends.whole(pg) : (pg + 1) * CACHE_TOKENS <= lim_min); };
     do {
-        for (; whole(); more = walk.next(pg, id, mine)) {
+        if constexpr (KIND == WHOLE) {
+            for (; whole(); more = walk.next(pg, id, mine)) {
+                page_data<D> x;
+                load_page<D>(x, page());
+                page_step<T, D, XT, false, SC>(x, nullptr, SC::ON ? pg * CACHE_TOKENS : 0, row, lim_max, qf, form, st, seen);
+            }
+        } else if (whole()) {
+            // the next page's keys are under way during this one's softmax, its values during its scores
             page_data<D> x;
-            load_page<D>(x, page());
-            page_step<T, D, XT, false, SC>(x, nullptr, SC::ON ? pg * CACHE_TOKENS : 0, row, lim_max, qf, form, st, seen);
+            load_keys<D>(x, page());
+            while (whole()) {
+                f32x4_t s[XT][4];
+                load_values<D>(x, page());
+                __builtin_amdgcn_sched_barrier(0);
+                page_scores<T, D, XT>(x, qf, s);
+                const int first = SC::ON ? pg * CACHE_TOKENS : 0;
+                more = walk.next(pg, id, mine);
+                if (whole()) load_keys<D>(x, page());
+                __builtin_amdgcn_sched_barrier(0);
+                page_weigh<T, D, XT, false, SC>(x, nullptr, first, row, lim_max, s, form, st, seen);
+            }
         }
         for (; more; more = walk.next(pg, id, mine)) {
             if (SC::ON && whole()) break;           // behind a window's first page

@@ -338,7 +338,10 @@ struct score_form {
     __device__ __forceinline__ void apply(V& s, const scored::row& w, int first, P place) const {
         if (capped) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = capped_of(s[i]);
+            for (int i = 0; i < N; ++i) {
+                s[i] = capped_of(s[i]);
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // few at a time: registers
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) s[i] *= scale;
@@ -346,7 +349,10 @@ struct score_form {
         if (sloped) {
             const float away = static_cast<float>(w.at - first);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[i] = fmaf(-w.slope, fabsf(away - static_cast<float>(place(i))), s[i]);
+            for (int i = 0; i < N; ++i) {
+                s[i] = fmaf(-w.slope, fabsf(away - static_cast<float>(place(i))), s[i]);
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
         }
     }
 };
@@ -580,11 +586,13 @@ __device__ __forceinline__ void page_scores(const page_data<D>& pd, const frag_b
     }
 }
 
-// The rest of a page: softmax and the product with the values.  MASKED: some row's limit,
-// or the list's end, may lie inside it.
-template <typename T, int D, int XT, bool MASKED, class SC>
+// The rest of a page: softmax and the product with the values.  masks: some row's limit, or the
+// list's end, may lie inside it; known where this is compiled for plain scores (a loop without
+// masks and one with them), at run time for others, whose masked pages come first and last: two
+// loops inside one cost the rows' registers a second time.
+template <typename T, int D, int XT, class SC>
 __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* page, int pos,
-                                           const typename SC::row (&row)[XT], int lim_max, f32x4_t (&s)[XT][4],
+                                           const typename SC::row (&row)[XT], int lim_max, bool masks, f32x4_t (&s)[XT][4],
                                            const form_of_t<T, SC>& form, tile_state<T, D> (&st)[XT], powers_seen& seen) {
     constexpr int NT = terms_of<T>;
     const int g = lane_id() >> 4;
@@ -599,16 +607,18 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
     const uint32_t four = at & 2 ? (at & 1 ? vw[3] : vw[2]) : (at & 1 ? vw[1] : vw[0]);
     uint32_t marked = ~0u;
     uint32_t bits[XT] = {}, together = 0;      // scored, masked: what this lane's row, and some row, sees of its tokens
-    if constexpr (MASKED && SC::ON) {
+    if (SC::ON && masks) {
+        if constexpr (SC::ON) {
 #pragma unroll
-        for (int x = 0; x < XT; ++x) {
+            for (int x = 0; x < XT; ++x) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) bits[x] |= seen_bits(row[x], pos + 16 * t + 4 * g) << (4 * t);
-            together |= bits[x];
+                for (int t = 0; t < 4; ++t) bits[x] |= seen_bits(row[x], pos + 16 * t + 4 * g) << (4 * t);
+                together |= bits[x];
+            }
         }
         together = lanes_or(together);
         marked = bytes_of((together >> (4 * at)) & 15u);
-    } else if constexpr (MASKED) {
+    } else if (masks) {
         marked = first_bytes(lim_max - (pos + 16 * at + 4 * g));
     }
     float mx[XT];
@@ -621,7 +631,7 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
             for (int t = 0; t < 4; ++t)
                 form.template apply<4>(s[x][t], row[x], pos + 4 * g, [t](int i) { return 16 * t + i; });
         }
-        if constexpr (MASKED) {
+        if (masks) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -679,6 +689,14 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
             for (int c = 0; c < D / 16; ++c) st[x].o[c] *= f;
         }
     }
+    if (SC::ON && masks) {
+        // what no row sees may hold any power: one that a weight of 0 leaves 0
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint32_t real = bytes_of((together >> (4 * t)) & 15u);
+            vw[t] = (vw[t] & real) | (static_cast<uint32_t>(seen.most) * 0x01010101u & ~real);
+        }
+    }
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         row_softmax_t<T>& w = st[x].w;
@@ -691,7 +709,7 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
                 sum += e;
                 // a masked place's power may be anything
                 const uint32_t byte = (vw[t] >> (8 * i)) & 0xffu;
-                p[t][i] = MASKED && e == 0.f ? 0.f : e * (NT == 1 ? seen.scaled(byte) : power_of(byte));
+                p[t][i] = !SC::ON && masks && e == 0.f ? 0.f : e * (NT == 1 ? seen.scaled(byte) : power_of(byte));
             }
         w.l = fmaf(sum, w.down, w.l);
 #pragma unroll
@@ -701,8 +719,8 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
             split_weights<NT>(pf[x][y], z);
         }
     }
-    uint32_t keep[4], any = 0;
-    if constexpr (MASKED) {
+    uint32_t keep[4] = {}, any = 0;
+    if (masks) {
         // Codes past every row's limit are whatever the page held: taken as
         // zeros.  A NaN below it, which some rows see and others do not, is
         // taken out of the product, too.
@@ -734,7 +752,7 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
                 st[x].o[c] = mma16(v1, pf[x][1][y], st[x].o[c]);
             }
     }
-    if constexpr (MASKED) {
+    if (masks) {
         // A NaN goes to the rows that see it, whatever their weight on it: a second product,
         // from the page's codes once more, counts it where a row's limit lies past it.
         if (__ballot(any != 0) == 0) return;
@@ -768,14 +786,14 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
     }
 }
 
-template <typename T, int D, int XT, bool MASKED, class SC>
+template <typename T, int D, int XT, class SC>
 __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos,
-                                          const typename SC::row (&row)[XT], int lim_max,
+                                          const typename SC::row (&row)[XT], int lim_max, bool masks,
                                           const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], const form_of_t<T, SC>& form,
                                           tile_state<T, D> (&st)[XT], powers_seen& seen) {
     f32x4_t s[XT][4];
     page_scores<T, D, XT>(pd, qf, s);
-    page_weigh<T, D, XT, MASKED, SC>(pd, page, pos, row, lim_max, s, form, st, seen);
+    page_weigh<T, D, XT, SC>(pd, page, pos, row, lim_max, masks, s, form, st, seen);
 }
 
 // Element offset of row r (query head and token of KV head h) in q or o.
@@ -884,37 +902,39 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
     int pg, id;
     bool more = walk.next(pg, id, mine);
     const auto page = [&]() { return a.c.pool + (static_cast<int64_t>(id) * a.c.heads + h) * cache_page_bytes(D); };
-    const auto whole = [&]() { return more && (SC::ON ? ends.whole(pg) : (pg + 1) * CACHE_TOKENS <= lim_min); };
-    do {
-        if constexpr (KIND == WHOLE) {
-            for (; whole(); more = walk.next(pg, id, mine)) {
-                page_data<D> x;
-                load_page<D>(x, page());
-                page_step<T, D, XT, false, SC>(x, nullptr, SC::ON ? pg * CACHE_TOKENS : 0, row, lim_max, qf, form, st, seen);
-            }
-        } else if (whole()) {
-            // the next page's keys are under way during this one's softmax, its values during its scores
-            page_data<D> x;
-            load_keys<D>(x, page());
-            while (whole()) {
-                f32x4_t s[XT][4];
-                load_values<D>(x, page());
-                __builtin_amdgcn_sched_barrier(0);
-                page_scores<T, D, XT>(x, qf, s);
-                const int first = SC::ON ? pg * CACHE_TOKENS : 0;
-                more = walk.next(pg, id, mine);
-                if (whole()) load_keys<D>(x, page());
-                __builtin_amdgcn_sched_barrier(0);
-                page_weigh<T, D, XT, false, SC>(x, nullptr, first, row, lim_max, s, form, st, seen);
-            }
-        }
+    const auto whole = [&]() { return more && (pg + 1) * CACHE_TOKENS <= lim_min; };
+    if constexpr (SC::ON) {
         for (; more; more = walk.next(pg, id, mine)) {
-            if (SC::ON && whole()) break;           // behind a window's first page
             page_data<D> x;
             load_page<D>(x, page());
-            page_step<T, D, XT, true, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, qf, form, st, seen);
+            page_step<T, D, XT, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, !ends.whole(pg), qf, form, st, seen);
         }
-    } while (SC::ON && more);
+    } else if constexpr (KIND == WHOLE) {
+        for (; whole(); more = walk.next(pg, id, mine)) {
+            page_data<D> x;
+            load_page<D>(x, page());
+            page_step<T, D, XT, SC>(x, nullptr, 0, row, lim_max, false, qf, form, st, seen);
+        }
+    } else if (whole()) {
+        // the next page's keys are under way during this one's softmax, its values during its scores
+        page_data<D> x;
+        load_keys<D>(x, page());
+        while (whole()) {
+            f32x4_t s[XT][4];
+            load_values<D>(x, page());
+            __builtin_amdgcn_sched_barrier(0);
+            page_scores<T, D, XT>(x, qf, s);
+            more = walk.next(pg, id, mine);
+            if (whole()) load_keys<D>(x, page());
+            __builtin_amdgcn_sched_barrier(0);
+            page_weigh<T, D, XT, SC>(x, nullptr, 0, row, lim_max, false, s, form, st, seen);
+        }
+    }
+    for (; !SC::ON && more; more = walk.next(pg, id, mine)) {
+        page_data<D> x;
+        load_page<D>(x, page());
+        page_step<T, D, XT, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, true, qf, form, st, seen);
+    }
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         float l = st[x].w.l;
@@ -1036,11 +1056,11 @@ __device__ __forceinline__ void rows_move(const f32x16_t (&s)[N], const float (*
         for (int i = 0; i < 16; ++i) st.o[c][i] *= f;
 }
 
-// One page in LDS for a wave's rows, where some row's limit, or the list's end,
-// may lie inside it.
+// One page in LDS for a wave's rows, where (plain scores) some row's limit, or the list's end,
+// may lie inside it, or (others) `masks` says so.
 template <typename T, int D, class SC>
 __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const float (*page_power)[2][64], int first,
-                                          const typename SC::row& row, int wmax,
+                                          const typename SC::row& row, int wmax, bool masks,
                                           const frag_bf16 (&qf)[D / 32][2][terms_of<T>], const form_of_t<T, SC>& form,
                                           powers_seen& seen, rows_state<T, D>& st) {
     const float (*power)[64] = *page_power;
@@ -1069,19 +1089,21 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             form.template apply<16>(s[t], row, first + 4 * h2, [t](int i) { return t * 32 + 8 * (i / 4) + i % 4; });
-        bits = half_bits(row, first + 4 * h2);
-        together = half_union(bits);
-    }
+        if (masks) {
+            bits = half_bits(row, first + 4 * h2);
+            together = half_union(bits);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if constexpr (SC::ON) {
-                if (!((bits >> (16 * t + i)) & 1u)) s[t][i] = -INFINITY;
-            } else {
-                if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= row.limit) s[t][i] = -INFINITY;
-            }
+                for (int i = 0; i < 16; ++i) s[t][i] = (bits >> (16 * t + i)) & 1u ? s[t][i] : -INFINITY;
         }
+    } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (first + t * 32 + 8 * (i / 4) + 4 * h2 + i % 4 >= row.limit) s[t][i] = -INFINITY;
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -1105,8 +1127,8 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
             const float pv[4] = {pw.x, pw.y, pw.z, pw.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // a masked place's power may be anything
-                y[4 * x + i] = y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
+                // a masked place's power may be anything (scored: not what is in LDS)
+                y[4 * x + i] = !SC::ON && y[4 * x + i] == 0.f ? 0.f : y[4 * x + i] * pv[i];
             }
         }
         split_weights<NT>(pf[t], y);
@@ -1119,7 +1141,20 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
         for (int x = 0; x < 2; ++x)
             keep[t][x] = SC::ON ? bytes_of((together >> (8 * t + 4 * x)) & 15u)
                                 : first_bytes(wmax - (first + 16 * t + 8 * x + 4 * h2));
-    // as in page_step: stale codes are zeros, a NaN goes to the rows that see it
+    // as in page_step: stale codes are zeros, a NaN goes to the rows that see it; scored: only
+    // where there is a NaN, the weight of the others is 0
+    bool odd = !SC::ON;
+    if (SC::ON && masks) {
+        uint32_t nans = 0;
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint4 v = *reinterpret_cast<const uint4*>(vp + c * 2048 + 512 * x);
+                nans |= nan_bytes(v.x) | nan_bytes(v.y) | nan_bytes(v.z) | nan_bytes(v.w);
+            }
+        odd = __ballot(nans != 0) != 0;
+    }
 #pragma unroll
     for (int c = 0; c < VC; ++c) {
         const uint4 va = *reinterpret_cast<const uint4*>(vp + c * 2048);
@@ -1127,12 +1162,14 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
         uint32_t w[4][2] = {{va.x, vb.x}, {va.y, vb.y}, {va.z, vb.z}, {va.w, vb.w}};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
+            if (odd) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                w[t][x] &= keep[t][x];
-                const uint32_t nan = nan_bytes(w[t][x]);
-                w[t][x] &= ~nan;
-                any |= nan;
+                for (int x = 0; x < 2; ++x) {
+                    w[t][x] &= keep[t][x];
+                    const uint32_t nan = nan_bytes(w[t][x]);
+                    w[t][x] &= ~nan;
+                    any |= nan;
+                }
             }
             weight_frag_t<T> vf;
             decode_values(vf, w[t][0], w[t][1]);
@@ -1168,12 +1205,10 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
 }
 
 // The two pages of a stage together, no limit inside either.
-template <typename T, int D, class SC>
+template <typename T, int D>
 __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase, const float (*power)[2][64],
-                                          const int (&first)[STAGE], const typename SC::row& row,
-                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], const form_of_t<T, SC>& form,
-                                          powers_seen& seen, rows_state<T, D>& st) {
-    const float scale = SC::ON ? 1.f : form.scale;
+                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale, powers_seen& seen,
+                                          rows_state<T, D>& st) {
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
     const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
     f32x16_t s[4];
@@ -1193,12 +1228,6 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
                 mma(s[t], k1, qf[w][1][y]);
             }
         }
-    }
-    if constexpr (SC::ON) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            form.template apply<16>(s[t], row, first[t / 2] + 4 * h2,
-                                    [t](int i) { return (t % 2) * 32 + 8 * (i / 4) + i % 4; });
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -1371,22 +1400,25 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
     // hand.  Past the barrier every wave is done with the other buffer.
     int at[STAGE];
     auto turn = [&]() {
+        uint32_t mine[STAGE];            // scored: is the lane's token seen by some row of the wave (all ones)?
+        if constexpr (SC::ON) {
+            // what lies between the rows' ranges may never have been written
+#pragma unroll
+            for (int x = 0; x < STAGE; ++x) {
+                mine[x] = x < have && wave_ends.whole(pos[x]) ? ~0u : 0u;
+                if (!mine[x] && x < have && wave_ends.sees(pos[x])) {
+                    const uint32_t here = half_union(half_bits(row, pos[x] * CACHE_TOKENS + 4 * h2));
+                    const uint32_t there = static_cast<uint32_t>(__shfl_xor(static_cast<int>(here), 32, 64));
+                    mine[x] = 0u - ((((lane >> 2) & 1) == h2 ? here : there) >> (4 * (lane >> 3) + (lane & 3)) & 1u);
+                }
+            }
+        }
         if constexpr (NT == 1) {
             uint32_t marked = 0;
 #pragma unroll
             for (int x = 0; x < STAGE; ++x) {
-                if constexpr (!SC::ON) {
-                    if (x < have && pos[x] * CACHE_TOKENS + lane < wmax) marked |= static_cast<uint32_t>(ve[x]) << (8 * x);
-                } else {
-                    // seen by some row: what lies between the rows' ranges may never have been written
-                    uint32_t mine = x < have && wave_ends.whole(pos[x]) ? ~0u : 0u;
-                    if (!mine && x < have && wave_ends.sees(pos[x])) {
-                        const uint32_t here = half_union(half_bits(row, pos[x] * CACHE_TOKENS + 4 * h2));
-                        const uint32_t there = static_cast<uint32_t>(__shfl_xor(static_cast<int>(here), 32, 64));
-                        mine = 0u - ((((lane >> 2) & 1) == h2 ? here : there) >> (4 * (lane >> 3) + (lane & 3)) & 1u);
-                    }
-                    marked |= (mine & ve[x]) << (8 * x);
-                }
+                if constexpr (SC::ON) marked |= (mine[x] & ve[x]) << (8 * x);
+                else if (x < have && pos[x] * CACHE_TOKENS + lane < wmax) marked |= static_cast<uint32_t>(ve[x]) << (8 * x);
             }
             seen.look(marked);
         }
@@ -1394,6 +1426,7 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
         for (int x = 0; x < STAGE; ++x) {
             power[wave][x][0][lane] = power_of(ke[x]);
             power[wave][x][1][lane] = NT == 1 ? seen.scaled(seen.raised(ve[x])) : power_of(ve[x]);
+            if (SC::ON && !mine[x]) power[wave][x][1][lane] = 1.f;      // any that a weight of 0 leaves 0
             at[x] = pos[x];
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -1402,30 +1435,24 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
         request(buf ^ 1);
         return n;
     };
-    const auto whole = [&]() {
-        if constexpr (SC::ON) return have == STAGE && ends.whole(pos[0]) && ends.whole(pos[STAGE - 1]);
-        else return have == STAGE && pos[STAGE - 1] < full;
-    };
-    do {
-        while (whole()) {
+    if constexpr (!SC::ON) {
+        while (have == STAGE && pos[STAGE - 1] < full) {
             turn();
-            const int first[STAGE] = {at[0] * CACHE_TOKENS, at[STAGE - 1] * CACHE_TOKENS};
-            rows_pair<T, D, SC>(codes[buf][0], kbase, vbase, power[wave], first, row, qf, form, seen, st);
+            rows_pair<T, D>(codes[buf][0], kbase, vbase, power[wave], qf, form.scale, seen, st);
             buf ^= 1;
         }
-        while (have > 0) {
-            if (SC::ON && whole()) break;           // behind a window's first pages
-            const int n = turn();
+    }
+    while (have > 0) {
+        const int n = turn();
 #pragma unroll 1
-            for (int x = 0; x < n; ++x) {
-                const int pg = x ? at[STAGE - 1] : at[0], first = pg * CACHE_TOKENS;
-                if (SC::ON ? wave_ends.sees(pg) : first < wmax)
-                    rows_step<T, D, SC>(codes[buf][x] + kbase, codes[buf][x] + vbase, &power[wave][x], first, row, wmax, qf,
-                                        form, seen, st);
-            }
-            buf ^= 1;
+        for (int x = 0; x < n; ++x) {
+            const int pg = x ? at[STAGE - 1] : at[0], first = pg * CACHE_TOKENS;
+            if (SC::ON ? wave_ends.sees(pg) : first < wmax)
+                rows_step<T, D, SC>(codes[buf][x] + kbase, codes[buf][x] + vbase, &power[wave][x], first, row, wmax,
+                                    SC::ON && !wave_ends.whole(pg), qf, form, seen, st);
         }
-    } while (SC::ON && have > 0);
+        buf ^= 1;
+    }
     f32x16_t(&o)[VC] = st.o;
     float m = st.w.m(), l = st.w.l;
     const float back = seen.back(st.w);

@@ -680,8 +680,8 @@ vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c
  *   span    device int32 [batch][n][2] or NULL.
  *   The rest is as for vsa2_attn_cache, what positions hold that no row sees reaches
  *   no output.  ws: vsa2_attn_cache_scored_workspace bytes for the same scores.
- * Errors: as for vsa2_attn_cache; cap, window or sink negative, cap not finite
- * (VSA2_ERR_VALUE).
+ * Errors: as for vsa2_attn_cache; a cap that is not 0 and outside 2^-20 to 2^20, a
+ * negative window or sink (VSA2_ERR_VALUE).
  */
 typedef struct {
     float cap;

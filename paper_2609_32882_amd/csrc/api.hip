@@ -261,7 +261,7 @@ vsa2_status check_attn_shared(const vsa2_cache* pre, const vsa2_cache* c, int32_
 // The options of a scored call.
 vsa2_status check_scores(const vsa2_scores* s) {
     if (!s) return VSA2_ERR_NULL;
-    if (!(s->cap >= 0.f) || s->cap > 3.402823466e38f) return VSA2_ERR_VALUE;
+    if (s->cap != 0.f && !(s->cap >= 0x1p-20f && s->cap <= 0x1p20f)) return VSA2_ERR_VALUE;
     if (s->window < 0 || s->sink < 0) return VSA2_ERR_VALUE;
     return VSA2_OK;
 }

@@ -304,12 +304,22 @@ struct scored_ends {
 };
 
 // The options' part of a score, in base 2: log2 e (cap tanh(x / cap) - slope |at - position|) of
-// x = s * scale.  tanh(y) = 1 - 2 / (e^2y + 1); with fp32 queries below 0.4 its series, where
-// the difference would cost bits (cap 50: 2^-17 of the weights).
+// x = s * scale.
+//
+// tanh(y) = 1 - 2 / (e^2y + 1), or, where all of a wave's |y| are at most 0.5, the odd polynomial
+// y + a y^3 + b y^5 + c y^7 that is nearest to it there (by linear programming over 3,001 points;
+// off by 2^-22.3 at most, which times the cap is what is left of a score's error): s times a
+// polynomial of s^2, the bias added by the same instructions.  fp32 queries take scores below 0.4
+// by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
+// of the weights).  A page that lies on one side of all rows' own positions has a bias that is
+// linear in the position.  1,792 tokens over 10,752, 12 heads: us without options, with a
+// cap of 30 (with scores past the polynomial:), with the bias , plain attention 152.
 template <bool EXACT>
 struct score_form {
     float scale, cap, rate;      // scale times log2 e, cap times log2 e, exponent of a score
     float cut;                   // scale / cap
+    float small;                 // scores below this take the polynomial
+    float c1, c2, c3;            // its factors of s^2, s^4, s^6, times scale (caps are 2^-20 to 2^20: all finite)
     bool capped, sloped;
     __device__ __forceinline__ score_form(const scored& sc, int D) {
         const float root = 1.f / sqrtf(static_cast<float>(D));
@@ -319,6 +329,11 @@ struct score_form {
         cap = sc.cap * LOG2E;
         cut = capped ? root / sc.cap : 0.f;
         rate = 2.f * LOG2E * cut;
+        small = 0.5f / cut;
+        const float u = cut * cut;
+        c1 = scale * u * -0.33326461f;
+        c2 = scale * u * u * 0.13185862f;
+        c3 = scale * u * u * u * -0.0442293f;
     }
     __device__ __forceinline__ float capped_of(float s) const {
         const float e = fast_exp2(EXACT ? fabsf(s) * rate : s * rate);
@@ -333,27 +348,62 @@ struct score_form {
         const float far = copysignf(cap * fmaf(-2.f, __builtin_amdgcn_rcpf(e + 1.f), 1.f), s);
         return fabsf(y) < 0.4f ? near : far;         // a NaN stays one
     }
-    // N scores at positions first + place(i)
-    template <int N, typename V, typename P>
-    __device__ __forceinline__ void apply(V& s, const scored::row& w, int first, P place) const {
-        if (capped) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                s[i] = capped_of(s[i]);
-                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // few at a time: registers
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[i] *= scale;
-        }
+    // The scores s[t][i], t below TILES, of the page at `first`, at positions here + place(t, i);
+    // returns what the results are still to be multiplied with (the same for all).
+    template <int TILES, int N, typename V, typename P>
+    __device__ __forceinline__ float apply(V* s, const scored::row& w, int first, int here, P place) const {
+        if (!capped && !sloped) return scale;
+        const float away = static_cast<float>(w.at - here);
+        float a = 0.f, slant = 0.f;             // a linear bias: a + slant * place
+        bool linear = true;
         if (sloped) {
-            const float away = static_cast<float>(w.at - first);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                s[i] = fmaf(-w.slope, fabsf(away - static_cast<float>(place(i))), s[i]);
-                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-            }
+            const bool before = w.at >= first + CACHE_TOKENS - 1, behind = w.at <= first;
+            linear = __ballot(!before && !behind) == 0;
+            slant = behind ? -w.slope : w.slope;
+            a = -slant * away;
         }
+        bool poly = !capped;
+        if (capped) {
+            float most = 0.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < N; i += 2) most = fmaxf(fmaxf(most, fabsf(s[t][i])), fabsf(s[t][i + 1]));
+            poly = !EXACT && __ballot(most >= small) == 0;          // (a NaN goes through either)
+        }
+        if (poly && linear) {
+            if (capped) {
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const float u = s[t][i] * s[t][i];
+                        s[t][i] = fmaf(s[t][i], fmaf(u, fmaf(u, fmaf(u, c3, c2), c1), scale), a);
+                    }
+            } else {
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s[t][i] = fmaf(s[t][i], scale, a);
+            }
+            if (!sloped) return 1.f;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[t][i] = fmaf(slant, static_cast<float>(place(t, i)), s[t][i]);
+            return 1.f;
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[t][i] = capped ? capped_of(s[t][i]) : s[t][i] * scale;
+        if (!sloped) return 1.f;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                s[t][i] = fmaf(-w.slope, fabsf(away - static_cast<float>(place(t, i))), s[t][i]);
+        return 1.f;
     }
 };
 // Plain scores: nothing but the scale, which the softmax applies.
@@ -596,7 +646,7 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
                                            const form_of_t<T, SC>& form, tile_state<T, D> (&st)[XT], powers_seen& seen) {
     constexpr int NT = terms_of<T>;
     const int g = lane_id() >> 4;
-    const float scale = SC::ON ? 1.f : form.scale;
+    float scale = form.scale;
     uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
     uint4 vr[D / 16];
 #pragma unroll
@@ -627,9 +677,7 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         if constexpr (SC::ON) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                form.template apply<4>(s[x][t], row[x], pos + 4 * g, [t](int i) { return 16 * t + i; });
+            scale = form.template apply<4, 4>(s[x], row[x], pos, pos + 4 * g, [](int t, int i) { return 16 * t + i; });
         }
         if (masks) {
 #pragma unroll
@@ -1064,7 +1112,7 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
                                           const frag_bf16 (&qf)[D / 32][2][terms_of<T>], const form_of_t<T, SC>& form,
                                           powers_seen& seen, rows_state<T, D>& st) {
     const float (*power)[64] = *page_power;
-    const float scale = SC::ON ? 1.f : form.scale;
+    float scale = form.scale;
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
     const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
     f32x16_t s[2];
@@ -1086,9 +1134,7 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
     }
     uint32_t bits = 0, together = 0;       // scored: what this lane's row, and some row, sees of its 32 tokens
     if constexpr (SC::ON) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            form.template apply<16>(s[t], row, first + 4 * h2, [t](int i) { return t * 32 + 8 * (i / 4) + i % 4; });
+        scale = form.template apply<2, 16>(s, row, first, first + 4 * h2, [](int t, int i) { return t * 32 + 8 * (i / 4) + i % 4; });
         if (masks) {
             bits = half_bits(row, first + 4 * h2);
             together = half_union(bits);
@@ -1205,10 +1251,12 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
 }
 
 // The two pages of a stage together, no limit inside either.
-template <typename T, int D>
+template <typename T, int D, class SC>
 __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase, const float (*power)[2][64],
-                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], float scale, powers_seen& seen,
-                                          rows_state<T, D>& st) {
+                                          const int (&pages)[STAGE], const typename SC::row& row,
+                                          const frag_bf16 (&qf)[D / 32][2][terms_of<T>], const form_of_t<T, SC>& form,
+                                          powers_seen& seen, rows_state<T, D>& st) {
+    float scale = form.scale;
     constexpr int NT = terms_of<T>, KC = D / 32, VC = D / 32;
     const int lane = lane_id(), h2 = lane >> 5, col = lane & 31;
     f32x16_t s[4];
@@ -1227,6 +1275,14 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
                 mma(s[t], k0, qf[w][0][y]);
                 mma(s[t], k1, qf[w][1][y]);
             }
+        }
+    }
+    if constexpr (SC::ON) {
+#pragma unroll
+        for (int x = 0; x < STAGE; ++x) {
+            const int first = pages[x] * CACHE_TOKENS;
+            scale = form.template apply<2, 16>(s + 2 * x, row, first, first + 4 * h2,
+                                       [](int t, int i) { return t * 32 + 8 * (i / 4) + i % 4; });
         }
     }
     float mx = -INFINITY;
@@ -1438,12 +1494,16 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
     if constexpr (!SC::ON) {
         while (have == STAGE && pos[STAGE - 1] < full) {
             turn();
-            rows_pair<T, D>(codes[buf][0], kbase, vbase, power[wave], qf, form.scale, seen, st);
+            rows_pair<T, D, SC>(codes[buf][0], kbase, vbase, power[wave], at, row, qf, form, seen, st);
             buf ^= 1;
         }
     }
     while (have > 0) {
-        const int n = turn();
+        int n = turn();
+        if (SC::ON && n == STAGE && wave_ends.whole(at[0]) && wave_ends.whole(at[STAGE - 1])) {
+            rows_pair<T, D, SC>(codes[buf][0], kbase, vbase, power[wave], at, row, qf, form, seen, st);
+            n = 0;
+        }
 #pragma unroll 1
         for (int x = 0; x < n; ++x) {
             const int pg = x ? at[STAGE - 1] : at[0], first = pg * CACHE_TOKENS;

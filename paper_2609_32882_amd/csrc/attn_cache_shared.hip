@@ -170,8 +170,11 @@ shared_plan plan_shared(int dtype, int D, const cache_view& pre, const cache_vie
     const bool pairs = !(dtype == 0 && D == 128);
     p.own.lists = static_cast<int64_t>(c.batch) * c.heads;
     p.pre.lists = static_cast<int64_t>(pre.batch) * c.heads;
+    // Shared rows in tiles of 32 up to 512 of them, else of 128, whose waves share the pages.  35,840
+    // shared tokens, 8 heads of 128, up to 512 own ones (us, tiles of 32 against 128): 130 rows 50
+    // and 69, 200 68 and 64, 240 76 and 85, 320 85 and 91, 640 147 and 138.
     p.own.tile_rows = own_rows <= 64 ? TILE : ROWS;
-    p.pre.tile_rows = own_rows > 64 || pre_rows > 256 ? ROWS : (pairs ? 2 * TILE : TILE);
+    p.pre.tile_rows = own_rows > 64 || pre_rows > 512 ? ROWS : (pairs ? 2 * TILE : TILE);
     const int64_t rows[2] = {pre_rows, own_rows}, pages[2] = {pre.max_pages, c.max_pages};
     side_plan* side[2] = {&p.pre, &p.own};
     int64_t most[2];

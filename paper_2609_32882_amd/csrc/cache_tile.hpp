@@ -1494,7 +1494,9 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
     if constexpr (!SC::ON) {
         while (have == STAGE && pos[STAGE - 1] < full) {
             turn();
-            rows_pair<T, D, SC>(codes[buf][0], kbase, vbase, power[wave], at, row, qf, form, seen, st);
+            // (a wave without rows: shared lists' last tile has few)
+            if (KIND != SHARED || wmax > 0)
+                rows_pair<T, D, SC>(codes[buf][0], kbase, vbase, power[wave], at, row, qf, form, seen, st);
             buf ^= 1;
         }
     }

@@ -19,7 +19,9 @@ CASES = [
     (2, 3, 6, 2, 64, 5, [300, 77], [5, 3, 70, 8, 130, 6], [5, 4, 0, 1, 5, 5], True, False, "f32"),
     (1, 20, 8, 2, 64, 1, [600], [7 * i for i in range(20)], None, False, True, "bf16"),
     (3, 1, 4, 4, 128, 16, [65, 0, 200], [16, 40, 100], None, True, False, "bf16"),
-    (1, 40, 8, 1, 64, 1, [257], [3 + i for i in range(40)], None, False, False, "bf16"),      # more than 256 rows
+    (1, 40, 8, 1, 64, 1, [257], [3 + i for i in range(40)], None, False, False, "bf16"),
+    (1, 70, 8, 1, 64, 1, [201], [2 + i % 9 for i in range(70)], None, False, False, "bf16"),  # more than 512 rows
+    (1, 19, 3, 1, 128, 10, [65], [12] * 19, None, True, False, "f32"),
     (1, 30, 3, 1, 128, 3, [129], [10] * 30, None, True, False, "f32"),
     (1, 2, 4, 2, 64, 40, [190], [64, 41], [40, 39], True, False, "bf16"),                     # many rows on both sides
     (2, 2, 2, 1, 128, 70, [128, 63], [70, 72, 100, 3], [70, 0, 70, 3], False, False, "bf16"),

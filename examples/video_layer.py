@@ -1,5 +1,5 @@
-"""One attention layer of a video model around the library, in training and in
-streaming generation, with random weights and inputs.
+"""One attention layer of a video model around the library, in training, in streaming
+generation and in sampling, with random weights and inputs.
 
 Training: projection -> per-head norm, (time, height, width) rotation and cube-
 major layout in one call -> pool -> route -> block-sparse attention -> its
@@ -8,6 +8,10 @@ gradients -> the projection's and the gains' gradients.
 Streaming: frames arrive in chunks.  A chunk's tokens stay in raster order
 (1 x 1 x 1 cubes), are rotated by their place in the clip, and go into a paged
 8-bit cache; the chunk then attends everything the cache holds.
+
+Sampling: several samples go on from one clip, whose keys and values are kept and read
+once for all of them.  A sample's own frames are in a list of its own; between chunks
+samples are picked to go on from, and only frames of a window stay.
 
     python examples/video_layer.py
 """
@@ -94,6 +98,50 @@ class Layer:
             vsa2.attn_cache(cache, q, start, o=o.transpose(1, 2))
             yield o.flatten(2)
 
+    def tokens(self, x, frames, h, w, rope):
+        """q, k, v [batch, heads, tokens, D] of projected rows in raster order, normalised and turned."""
+        q, k, v = self.split(x @ self.w_qkv)
+        q, k, _ = vsa2.qk_norm_rope(self.problem(x.shape[0], (frames, h, w), 1), q, k, q_gain=self.q_gain, k_gain=self.k_gain,
+                                    rope=rope, eps=self.eps)
+        return q, k, v
+
+    def sample(self, clip, chunks, picks, grid, window):
+        """clip [1, frames * h * w, width] is what all samples go on from; chunks [samples, h * w,
+        width] are one new frame of each, picks[i] (int32 [samples]) the sample whose own
+        frames each goes on from at chunk i, window the own frames that are kept.  Yields each
+        chunk's attention output [samples, tokens, heads_q * D]."""
+        samples, (frames, h, w) = chunks[0].shape[0], grid
+        old, n = clip.shape[1] // (h * w), h * w
+        ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        page = lambda tokens: -(-tokens // 64)
+        # one pool for both tables: the clip's list, and the samples' own ones
+        clip_pages, own_pages = page(old * n), page((window + 1) * n) + 1
+        total = clip_pages + samples * (own_pages + 2)
+        table = torch.full((1, clip_pages), -1, dtype=torch.int32, device="cuda")
+        prefix = vsa2.KVCache.empty(table, total, self.heads_kv, self.head_dim)
+        own = vsa2.KVCache(prefix.pool, torch.full((samples, own_pages), -1, dtype=torch.int32, device="cuda"))
+        refs = torch.zeros(total, dtype=torch.int32, device="cuda")
+        _, k, v = self.tokens(clip, old, h, w, self.rope(grid))
+        room = vsa2.cache_assign(prefix, refs, ints(0), count=ints(old * n))
+        vsa2.cache_write(prefix, k, v, ints(0), room)
+        length, count = torch.zeros(samples, dtype=torch.int32, device="cuda"), ints(n).expand(samples).contiguous()
+        origin = torch.zeros(samples, 3, dtype=torch.int32, device="cuda")
+        origin[:, 0] = old
+        rope = self.rope(grid, origin)
+        for x, pick in zip(chunks, picks):
+            # whole pages that the window has passed leave the lists
+            passed = torch.clamp(length - (window - 1) * n, min=0) // 64
+            length -= passed * 64
+            drop = torch.stack([torch.zeros_like(passed), passed], 1)
+            q, k, v = self.tokens(x, 1, h, w, rope)
+            room = vsa2.cache_assign(own, refs, length, source=pick, drop=drop, count=count)
+            vsa2.cache_write(own, k, v, length, room)
+            length += n
+            origin[:, 0] += 1
+            o = torch.empty(samples, n, self.heads_q, self.head_dim, dtype=x.dtype, device="cuda")
+            vsa2.attn_cache_shared(prefix, own, q, ints(old * n), length, o=o.transpose(1, 2))
+            yield o.flatten(2)
+
 
 def main():
     layer, grid = Layer(), (8, 16, 16)
@@ -106,6 +154,10 @@ def main():
           (tuple(o.shape), dw.float().norm(), dq_gain.norm(), dk_gain.norm()))
     for i, y in enumerate(layer.stream(x.split([1 * 256, 3 * 256, 4 * 256], 1), grid)):
         print("chunk %d: %d tokens, |output| %.3g" % (i, y.shape[1], y.float().norm()))
+    frames = [torch.randn(4, 256, width, generator=g, device="cuda").to(layer.dtype) for _ in range(3)]
+    picks = [torch.tensor(p, dtype=torch.int32, device="cuda") for p in ((0, 1, 2, 3), (0, 0, 3, 3), (1, 1, 1, 2))]
+    for i, y in enumerate(layer.sample(x[:, :5 * 256], frames, picks, grid, 2)):
+        print("samples' frame %d: |output| %.3g" % (i, y.float().norm()))
 
 
 if __name__ == "__main__":

@@ -42,12 +42,12 @@ struct scored_kernels {
     }
 };
 
-// The pages that a tile's rows may see at most, for the plan: with a window, that of its
+// The pages that a call's rows may see at most, for the plan: with a window, that of its
 // tokens together and the first positions.
 cache_view window_view(const cache_view& c, int n, int window, int sink) {
     cache_view v = c;
     if (window) {
-        const int64_t most = static_cast<int64_t>(window) + std::min(n, ROWS) + 2 * CACHE_TOKENS + sink + CACHE_TOKENS;
+        const int64_t most = static_cast<int64_t>(window) + n + 2 * CACHE_TOKENS + sink + CACHE_TOKENS;
         v.max_pages = static_cast<int>(std::min<int64_t>(c.max_pages, most / CACHE_TOKENS));
     }
     return v;

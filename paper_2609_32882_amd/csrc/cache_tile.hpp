@@ -312,8 +312,10 @@ struct scored_ends {
 // polynomial of s^2, the bias added by the same instructions.  fp32 queries take scores below 0.4
 // by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
 // of the weights).  A page that lies on one side of all rows' own positions has a bias that is
-// linear in the position.  1,792 tokens over 10,752, 12 heads: us without options, with a
-// cap of 30 (with scores past the polynomial:), with the bias , plain attention 152.
+// linear in the position.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
+// (plain attention 152), 161 with a bias, 185 with a cap that the polynomial serves, 204 with
+// one that it does not (by it alone the capped frame of attn_cache_scored.hip went from 222 to
+// 212 us).
 template <bool EXACT>
 struct score_form {
     float scale, cap, rate;      // scale times log2 e, cap times log2 e, exponent of a score
@@ -588,34 +590,32 @@ struct page_data {
     uint32_t ke;
 };
 template <int D>
-__device__ __forceinline__ void load_keys(page_data<D>& pd, const char* page) {
+__device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
     const int lane = lane_id();
     const uint4* kp = reinterpret_cast<const uint4*>(page) + lane;
+    const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
 #pragma unroll
     for (int i = 0; i < 4 * (D / 64); ++i) pd.k[i] = kp[i * 64];
     pd.ke = *reinterpret_cast<const uint32_t*>(page + 128 * D + (lane & 15) * 4);
-}
-template <int D>
-__device__ __forceinline__ void load_values(page_data<D>& pd, const char* page) {
-    const int lane = lane_id();
-    const uint4* vp = reinterpret_cast<const uint4*>(page + 64 * D) + lane;
     pd.ve = *reinterpret_cast<const uint4*>(page + 128 * D + 64 + (lane >> 4) * 16);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) pd.v[i] = vp[i * 64];
-}
-template <int D>
-__device__ __forceinline__ void load_page(page_data<D>& pd, const char* page) {
-    load_keys<D>(pd, page);
-    load_values<D>(pd, page);
     // all of them requested before the first is waited for
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// S^T of one page for XT tiles, its keys decoded once for all of them.
-template <typename T, int D, int XT>
-__device__ __forceinline__ void page_scores(const page_data<D>& pd, const frag_bf16 (&qf)[XT][D / 32][terms_of<T>],
-                                            f32x4_t (&s)[XT][4]) {
+// One page for XT tiles, decoded once for all of them.  masks: some row's limit, or the list's
+// end, may lie inside it; known where this is compiled for plain scores (a loop without masks
+// and one with them), at run time for others, whose masked pages come first and last: two loops
+// inside one cost the rows' registers a second time.
+template <typename T, int D, int XT, class SC>
+__device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos,
+                                          const typename SC::row (&row)[XT], int lim_max, bool masks,
+                                          const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], const form_of_t<T, SC>& form,
+                                          tile_state<T, D> (&st)[XT], powers_seen& seen) {
     constexpr int NT = terms_of<T>;
+    const int g = lane_id() >> 4;
+    f32x4_t s[XT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const float power = power_of((pd.ke >> (8 * t)) & 0xffu);
@@ -634,18 +634,6 @@ __device__ __forceinline__ void page_scores(const page_data<D>& pd, const frag_b
                 }
         }
     }
-}
-
-// The rest of a page: softmax and the product with the values.  masks: some row's limit, or the
-// list's end, may lie inside it; known where this is compiled for plain scores (a loop without
-// masks and one with them), at run time for others, whose masked pages come first and last: two
-// loops inside one cost the rows' registers a second time.
-template <typename T, int D, int XT, class SC>
-__device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* page, int pos,
-                                           const typename SC::row (&row)[XT], int lim_max, bool masks, f32x4_t (&s)[XT][4],
-                                           const form_of_t<T, SC>& form, tile_state<T, D> (&st)[XT], powers_seen& seen) {
-    constexpr int NT = terms_of<T>;
-    const int g = lane_id() >> 4;
     float scale = form.scale;
     uint32_t vw[4] = {pd.ve.x, pd.ve.y, pd.ve.z, pd.ve.w};
     uint4 vr[D / 16];
@@ -834,16 +822,6 @@ __device__ __forceinline__ void page_weigh(const page_data<D>& pd, const char* p
     }
 }
 
-template <typename T, int D, int XT, class SC>
-__device__ __forceinline__ void page_step(const page_data<D>& pd, const char* page, int pos,
-                                          const typename SC::row (&row)[XT], int lim_max, bool masks,
-                                          const frag_bf16 (&qf)[XT][D / 32][terms_of<T>], const form_of_t<T, SC>& form,
-                                          tile_state<T, D> (&st)[XT], powers_seen& seen) {
-    f32x4_t s[XT][4];
-    page_scores<T, D, XT>(pd, qf, s);
-    page_weigh<T, D, XT, SC>(pd, page, pos, row, lim_max, masks, s, form, st, seen);
-}
-
 // Element offset of row r (query head and token of KV head h) in q or o.
 template <rows_kind KIND = WHOLE>
 __device__ __forceinline__ int64_t row_offset(const row_view& v, const attn_args& a, int b, int h, int r) {
@@ -957,31 +935,17 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
             load_page<D>(x, page());
             page_step<T, D, XT, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, !ends.whole(pg), qf, form, st, seen);
         }
-    } else if constexpr (KIND == WHOLE) {
+    } else {
         for (; whole(); more = walk.next(pg, id, mine)) {
             page_data<D> x;
             load_page<D>(x, page());
             page_step<T, D, XT, SC>(x, nullptr, 0, row, lim_max, false, qf, form, st, seen);
         }
-    } else if (whole()) {
-        // the next page's keys are under way during this one's softmax, its values during its scores
-        page_data<D> x;
-        load_keys<D>(x, page());
-        while (whole()) {
-            f32x4_t s[XT][4];
-            load_values<D>(x, page());
-            __builtin_amdgcn_sched_barrier(0);
-            page_scores<T, D, XT>(x, qf, s);
-            more = walk.next(pg, id, mine);
-            if (whole()) load_keys<D>(x, page());
-            __builtin_amdgcn_sched_barrier(0);
-            page_weigh<T, D, XT, SC>(x, nullptr, 0, row, lim_max, false, s, form, st, seen);
+        for (; more; more = walk.next(pg, id, mine)) {
+            page_data<D> x;
+            load_page<D>(x, page());
+            page_step<T, D, XT, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, true, qf, form, st, seen);
         }
-    }
-    for (; !SC::ON && more; more = walk.next(pg, id, mine)) {
-        page_data<D> x;
-        load_page<D>(x, page());
-        page_step<T, D, XT, SC>(x, page(), pg * CACHE_TOKENS, row, lim_max, true, qf, form, st, seen);
     }
 #pragma unroll
     for (int x = 0; x < XT; ++x) {

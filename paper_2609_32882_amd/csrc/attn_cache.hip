@@ -26,6 +26,9 @@
 // TB/s.  For many rows bound by vector instructions, which hardly overlap with the
 // MFMAs of two waves a SIMD: 1,792 tokens over 35,840, 12 heads, 430 us, 0.92
 // PFLOP/s; vector unit busy 63% of the cycles and MFMAs 43%, waits for LDS 1%.
+//
+// The waves' code is in cache_tile.hpp; this file holds the kernels around it and the rules
+// by which a call is cut.
 #include <algorithm>
 
 #include "cache_tile.hpp"

@@ -26,6 +26,9 @@ CASES = [
     (1, 2, 4, 2, 64, 40, [190], [64, 41], [40, 39], True, False, "bf16"),                     # many rows on both sides
     (2, 2, 2, 1, 128, 70, [128, 63], [70, 72, 100, 3], [70, 0, 70, 3], False, False, "bf16"),
     (1, 3, 1, 1, 128, 66, [150], [66, 70, 1], [66, 66, 1], True, False, "f32"),
+    (2, 2, 2, 1, 64, 64, [70, 1], [64, 0, 100, 64], [64, 0, 10, 64], False, True, "bf16"),
+    (1, 2, 1, 1, 64, 100, [0], [150, 100], None, True, False, "bf16"),                        # nothing shared
+    (1, 2, 2, 1, 128, 150, [700], [200, 513], None, True, False, "bf16"),
     (1, 5, 2, 1, 128, 1, [2300], [100, 0, 64, 1, 33], None, False, False, "bf16"),            # a list in many pieces
 ]
 IDS = ["%dx%d-%d/%d-D%d-n%d-%s%s-%s" % (*c[:6], "_".join(map(str, c[6])), "-causal" if c[9] else "", c[11]) for c in CASES]

@@ -674,8 +674,8 @@ vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c
  *   j < sink,  or  j > p - window  and  span[b][i][0] <= j < span[b][i][1]
  * (window = 0, span NULL: all).  A window behind some first tokens; documents, each
  * token's own [from, to); a prefix that sees itself whole, [0, max(prefix, p + 1)) with
- * causal = 0.  The window also ends lists that lose their oldest pages: pages that no row
- * sees are not visited.
+ * causal = 0.  Pages between the first tokens and the rows'
+ * ranges are not visited.
  *   slope   device fp32 [heads_q], finite, or NULL.
  *   span    device int32 [batch][n][2] or NULL.
  *   The rest is as for vsa2_attn_cache, what positions hold that no row sees reaches

@@ -674,9 +674,8 @@ vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c
  *   j < sink,  or  j > p - window  and  span[b][i][0] <= j < span[b][i][1]
  * (window = 0, span NULL: all).  A window behind some first tokens; documents, each
  * token's own [from, to); a prefix that sees itself whole, [0, max(prefix, p + 1)) with
- * causal = 0.  Pages between the first tokens and the rows'
- * ranges are not visited.
- *   slope   device fp32 [heads_q], finite, or NULL.
+ * causal = 0.  Pages between the first tokens and the rows' ranges are not visited.
+ *   slope   device fp32 [heads_q], of sizes up to 2^90, or NULL.
  *   span    device int32 [batch][n][2] or NULL.
  *   The rest is as for vsa2_attn_cache, what positions hold that no row sees reaches
  *   no output.  ws: vsa2_attn_cache_scored_workspace bytes for the same scores.
@@ -713,6 +712,7 @@ vsa2_status vsa2_attn_cache_scored(const vsa2_cache* c, const vsa2_scores* score
  * Each gets the free page of the lowest index, and refs 1; none is left: -1, and a page that
  * could not be copied stays shared.  room[b] = how many of the count[b] tokens have a place
  * that is the sequence's alone: the count to give vsa2_cache_write with start = length.
+ * Calls that share refs or the pool run one after the other.
  *   c       the cache; c->table is `table`, table_heads is 1.  pool: copied pages are written.
  *   table   device int32 [batch][max_pages], read and written.
  *   refs    device int32 [pages], 16-byte aligned, read and written.  A new pool: zeros, and

@@ -306,10 +306,13 @@ struct scored_ends {
 // The options' part of a score, in base 2: log2 e (cap tanh(x / cap) - slope |at - position|) of
 // x = s * scale.
 //
-// tanh(y) = 1 - 2 / (e^2y + 1), or, where all of a wave's |y| are at most 0.5, the odd polynomial
-// y + a y^3 + b y^5 + c y^7 that is nearest to it there (by linear programming over 3,001 points;
-// off by 2^-22.3 at most, which times the cap is what is left of a score's error): s times a
-// polynomial of s^2, the bias added by the same instructions.  fp32 queries take scores below 0.4
+// tanh(y) = 1 - 2 / (e^2y + 1), or, below 0.5, the odd polynomial y + a y^3 + b y^5 + c y^7 that is
+// nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most): s times a
+// polynomial of s^2.  Where all of a wave's scores are small only that is worked out, the bias added
+// by the same instructions.  Elsewhere the first serves all of the wave's scores up to caps of 2^8,
+// off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a score takes the one
+// that is its own above, where small ones would lose bits (0.08 of a score of 1 at a cap of 2^20);
+// that for all caps took 238 us of the capped frame below instead of 204.  fp32 queries take scores below 0.4
 // by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
 // of the weights).  A page that lies on one side of all rows' own positions has a bias that is
 // linear in the position.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
@@ -336,6 +339,11 @@ struct score_form {
         c1 = scale * u * -0.33326461f;
         c2 = scale * u * u * 0.13185862f;
         c3 = scale * u * u * u * -0.0442293f;
+    }
+    // the polynomial, and the bias
+    __device__ __forceinline__ float small_of(float s, float bias) const {
+        const float u = s * s;
+        return fmaf(s, fmaf(u, fmaf(u, fmaf(u, c3, c2), c1), scale), bias);
     }
     __device__ __forceinline__ float capped_of(float s) const {
         const float e = fast_exp2(EXACT ? fabsf(s) * rate : s * rate);
@@ -378,10 +386,7 @@ struct score_form {
 #pragma unroll
                 for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const float u = s[t][i] * s[t][i];
-                        s[t][i] = fmaf(s[t][i], fmaf(u, fmaf(u, fmaf(u, c3, c2), c1), scale), a);
-                    }
+                    for (int i = 0; i < N; ++i) s[t][i] = small_of(s[t][i], a);
             } else {
 #pragma unroll
                 for (int t = 0; t < TILES; ++t)
@@ -395,10 +400,20 @@ struct score_form {
                 for (int i = 0; i < N; ++i) s[t][i] = fmaf(slant, static_cast<float>(place(t, i)), s[t][i]);
             return 1.f;
         }
+        if (!EXACT && cap > 256.f * LOG2E) {
 #pragma unroll
-        for (int t = 0; t < TILES; ++t)
+            for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[t][i] = capped ? capped_of(s[t][i]) : s[t][i] * scale;
+                for (int i = 0; i < N; ++i) {
+                    const float far = capped_of(s[t][i]);
+                    s[t][i] = fabsf(s[t][i]) < small ? small_of(s[t][i], 0.f) : far;         // a NaN stays one
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[t][i] = capped ? capped_of(s[t][i]) : s[t][i] * scale;
+        }
         if (!sloped) return 1.f;
 #pragma unroll
         for (int t = 0; t < TILES; ++t)

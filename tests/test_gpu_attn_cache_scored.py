@@ -147,6 +147,45 @@ def test_without_options_it_is_the_plain_attention(i):
     check(run(case, x[0], x, opt), ref.attn_reference(*x[:3], x[3], x[4], case[8]), case, opt)
 
 
+@pytest.mark.parametrize("n", [3, 130])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [0.0, 2.0 ** -20, 2.0 ** 20])
+def test_slopes_and_caps_at_their_ends(n, dtype, cap):
+    """A slope of 2^90 leaves the token itself, its weight 1 and its score the lse; -2^90 the list's first."""
+    case = (2, 4, 2, 64, n, 5, [290, 201], None, True, False, dtype)
+    x = make(case)
+    opt = dict(cap=cap, slope=torch.tensor([2.0 ** 90, -2.0 ** 90, 2.0 ** 90, 0.0]), window=0, sink=0, span=None)
+    o, lse = (y.double().cpu() for y in run(case, x[0], x, opt))
+    wo, wl, weight, logit = pref.scored_reference(*x[:5], case[8], **opt)
+    # one term: the weight's fp16 (2^-11) and the result's rounding, or three bf16 terms of the weight, their
+    # products' sum, the reciprocal and its product, some 2^-24 each
+    step = 2.0 ** -8 + 2.0 ** -10 if dtype == "bf16" else 2.0 ** -21
+    assert ((o - wo).abs()[:, :3] <= step * wo.abs()[:, :3]).all()
+    # own scores: the product's error and that of log2 e and back; far ones: the distance's product
+    delta = 2.0 ** -20 * logit[..., 0] + 2.0 ** -21 * (1 + wl.abs() + min(cap, 64.0))
+    assert ((lse - wl).abs() <= delta).all()
+    # without a slope the cap alone (errors as in check)
+    bound = step * wo.abs() + ((2.0 ** -8 if dtype == "bf16" else 0) + 2 * delta[..., None] + 2.0 ** -19) * weight
+    assert ((o - wo).abs() <= bound)[:, 3].all()
+
+
+@pytest.mark.parametrize("n", [3, 130])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_scores_beside_large_ones(n, dtype):
+    """A token whose scores pass half of a large cap takes no bits from the others of its tile."""
+    case = (1, 2, 1, 64, n, 5, [290], None, False, False, dtype)
+    x = make(case)
+    x[2][:, :, 0] *= 2.0 ** 14
+    opt = dict(cap=2.0 ** 14, slope=None, window=0, sink=0, span=None)
+    o, lse = (y.double().cpu() for y in run(case, x[0], x, opt))
+    wo, wl, weight, logit = pref.scored_reference(*x[:5], case[8], **opt)
+    delta = 2.0 ** -20 * logit + 2.0 ** -21             # without a part of the cap: the polynomial's is relative
+    bound = (2.0 ** -8 * (1 + 2.0 ** -6) * wo.abs() if dtype == "bf16" else 0) + (
+        (2.0 ** -8 if dtype == "bf16" else 0) + 2 * delta + 2.0 ** -19) * weight
+    assert ((o - wo).abs() <= bound)[:, :, 1:].all()
+    assert ((lse - wl).abs() <= delta[..., 0] + 2.0 ** -21 * (1 + wl.abs()))[:, :, 1:].all()
+
+
 @pytest.mark.parametrize("n", [4, 150])
 @pytest.mark.parametrize("which", [0, 1])
 def test_nan_reaches_only_the_rows_that_see_it(n, which):

@@ -312,11 +312,11 @@ struct scored_ends {
 // by the same instructions.  Elsewhere the first serves all of the wave's scores up to caps of 2^8,
 // off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a score takes the one
 // that is its own above, where small ones would lose bits (0.08 of a score of 1 at a cap of 2^20);
-// that for all caps took 238 us of the capped frame below instead of 204.  fp32 queries take scores below 0.4
+// that for all caps took 238 us of the capped frame below instead of 202.  fp32 queries take scores below 0.4
 // by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
 // of the weights).  A page that lies on one side of all rows' own positions has a bias that is
 // linear in the position.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
-// (plain attention 152), 161 with a bias, 185 with a cap that the polynomial serves, 204 with
+// (plain attention 152), 161 with a bias, 183 with a cap that the polynomial serves, 202 with
 // one that it does not (by it alone the capped frame of attn_cache_scored.hip went from 222 to
 // 212 us).
 template <bool EXACT>

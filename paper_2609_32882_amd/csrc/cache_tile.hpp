@@ -314,8 +314,9 @@ struct scored_ends {
 // that is its own above, where small ones would lose bits (0.08 of a score of 1 at a cap of 2^20);
 // that for all caps took 238 us of the capped frame below instead of 202.  fp32 queries take scores below 0.4
 // by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
-// of the weights).  A page that lies on one side of all rows' own positions has a bias that is
-// linear in the position.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
+// of the weights).  A page behind all rows' own positions, or more than a page before them, has a
+// bias that is linear in the position; nearer ones take distances as whole numbers, so that an own
+// position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
 // (plain attention 152), 161 with a bias, 183 with a cap that the polynomial serves, 202 with
 // one that it does not (by it alone the capped frame of attn_cache_scored.hip went from 222 to
 // 212 us).
@@ -367,7 +368,8 @@ struct score_form {
         float a = 0.f, slant = 0.f;             // a linear bias: a + slant * place
         bool linear = true;
         if (sloped) {
-            const bool before = w.at >= first + CACHE_TOKENS - 1, behind = w.at <= first;
+            // a page away at least: a, which the last terms take back, is twice the bias there at most
+            const bool before = w.at >= first + 2 * CACHE_TOKENS - 1, behind = w.at <= first;
             linear = __ballot(!before && !behind) == 0;
             slant = behind ? -w.slope : w.slope;
             a = -slant * away;

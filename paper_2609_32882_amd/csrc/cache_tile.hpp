@@ -308,18 +308,18 @@ struct scored_ends {
 //
 // tanh(y) = 1 - 2 / (e^2y + 1), or, below 0.5, the odd polynomial y + a y^3 + b y^5 + c y^7 that is
 // nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most): s times a
-// polynomial of s^2.  Where all of a wave's scores are small only that is worked out, the bias added
-// by the same instructions.  Elsewhere the first serves all of the wave's scores up to caps of 2^8,
-// off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a score takes the one
-// that is its own above, where small ones would lose bits (0.08 of a score of 1 at a cap of 2^20);
-// that for all caps took 238 us of the capped frame below instead of 202.  fp32 queries take scores below 0.4
-// by the series instead, the others as above: the difference would cost them bits (cap 50: 2^-17
-// of the weights).  A page behind all rows' own positions, or more than a page before them, has a
-// bias that is linear in the position; nearer ones take distances as whole numbers, so that an own
-// position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128: 150 us without options
-// (plain attention 152), 161 with a bias, 183 with a cap that the polynomial serves, 202 with
-// one that it does not (by it alone the capped frame of attn_cache_scored.hip went from 222 to
-// 212 us).
+// polynomial of s^2.  Where all of a wave's scores that some row sees are small only that is worked
+// out, the bias added by the same instructions.  Elsewhere the first serves all of the wave's scores
+// up to caps of 2^8, off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a
+// score takes the one that is its own above, where small ones would lose bits (0.08 of a score of 1
+// at a cap of 2^20); that for all caps took 238 us of the capped frame below instead of 202.  fp32
+// queries take scores below 0.4 by the series instead, the others as above: the difference would cost
+// them bits (cap 50: 2^-17 of the weights).  A page behind all rows' own positions, or more than a
+// page before them, has a bias that is linear in the position; nearer ones take distances as whole
+// numbers, so that an own position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128:
+// 150 us without options (plain attention 152), 161 with a bias, 183 with a cap that the polynomial
+// serves, 202 with one that it does not (by it alone the capped frame of attn_cache_scored.hip went
+// from 222 to 212 us).
 template <bool EXACT>
 struct score_form {
     float scale, cap, rate;      // scale times log2 e, cap times log2 e, exponent of a score
@@ -360,9 +360,11 @@ struct score_form {
         return fabsf(y) < 0.4f ? near : far;         // a NaN stays one
     }
     // The scores s[t][i], t below TILES, of the page at `first`, at positions here + place(t, i);
+    // masks: those without their bit in `bits` (N t + i) may be anything, and choose no form for the others;
     // returns what the results are still to be multiplied with (the same for all).
     template <int TILES, int N, typename V, typename P>
-    __device__ __forceinline__ float apply(V* s, const scored::row& w, int first, int here, P place) const {
+    __device__ __forceinline__ float apply(V* s, const scored::row& w, int first, int here, bool masks, uint32_t bits,
+                                           P place) const {
         if (!capped && !sloped) return scale;
         const float away = static_cast<float>(w.at - here);
         float a = 0.f, slant = 0.f;             // a linear bias: a + slant * place
@@ -381,6 +383,17 @@ struct score_form {
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
                 for (int i = 0; i < N; i += 2) most = fmaxf(fmaxf(most, fabsf(s[t][i])), fabsf(s[t][i + 1]));
+            if (masks) {
+                most = 0.f;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        int seen = static_cast<int>(bits << (31 - (N * t + i))) >> 31;
+                        asm("" : "+v"(seen));          // kept in a vector register: as many masks would not fit the scalar ones
+                        most = fmaxf(most, fabsf(__uint_as_float(__float_as_uint(s[t][i]) & static_cast<uint32_t>(seen))));
+                    }
+            }
             poly = !EXACT && __ballot(most >= small) == 0;          // (a NaN goes through either)
         }
         if (poly && linear) {
@@ -682,7 +695,7 @@ __device__ __forceinline__ void page_step(const page_data<D>& pd, const char* pa
 #pragma unroll
     for (int x = 0; x < XT; ++x) {
         if constexpr (SC::ON) {
-            scale = form.template apply<4, 4>(s[x], row[x], pos, pos + 4 * g, [](int t, int i) { return 16 * t + i; });
+            scale = form.template apply<4, 4>(s[x], row[x], pos, pos + 4 * g, masks, bits[x], [](int t, int i) { return 16 * t + i; });
         }
         if (masks) {
 #pragma unroll
@@ -1115,10 +1128,13 @@ __device__ __forceinline__ void rows_step(const char* kp, const char* vp, const 
     }
     uint32_t bits = 0, together = 0;       // scored: what this lane's row, and some row, sees of its 32 tokens
     if constexpr (SC::ON) {
-        scale = form.template apply<2, 16>(s, row, first, first + 4 * h2, [](int t, int i) { return t * 32 + 8 * (i / 4) + i % 4; });
         if (masks) {
             bits = half_bits(row, first + 4 * h2);
             together = half_union(bits);
+        }
+        scale = form.template apply<2, 16>(s, row, first, first + 4 * h2, masks, bits,
+                                           [](int t, int i) { return t * 32 + 8 * (i / 4) + i % 4; });
+        if (masks) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -1262,7 +1278,7 @@ __device__ __forceinline__ void rows_pair(const char* lds, int kbase, int vbase,
 #pragma unroll
         for (int x = 0; x < STAGE; ++x) {
             const int first = pages[x] * CACHE_TOKENS;
-            scale = form.template apply<2, 16>(s + 2 * x, row, first, first + 4 * h2,
+            scale = form.template apply<2, 16>(s + 2 * x, row, first, first + 4 * h2, false, 0,
                                        [](int t, int i) { return t * 32 + 8 * (i / 4) + i % 4; });
         }
     }

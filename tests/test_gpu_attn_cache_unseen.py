@@ -1,0 +1,57 @@
+"""What no row sees reaches no bit of the attentions' results: equal calls on pools whose stale
+bytes differ (behind a list's end, between two rows' ranges) give equal outputs.  NaN there is
+tested elsewhere; these are finite bytes of other requests."""
+import pytest
+import torch
+
+import around_reference as ref
+from test_gpu_attn_cache import make
+from test_gpu_attn_cache_scored import options, run, seen
+
+pytestmark = pytest.mark.gpu
+
+# (code, power) of stale places: a fresh page's zeros, the largest finite code, sizes as real ones have
+STALE = [(0x00, 0), (0x7e, 150), (0xb1, 118)]
+
+
+def filled(pool, table, D, unseen, code, power):
+    """The pool with the places in unseen bool [batch, positions] holding this code and power."""
+    pool = pool.clone()
+    for b, pos in unseen.nonzero().tolist():
+        for h in range(pool.shape[1]):
+            page = ref.page_for(table, b, h, pos, pool.shape[0])
+            if page is None:
+                continue
+            for x, at in enumerate(ref.offsets(pos % 64, D)):
+                pool[page, h, at] = code if x < 2 else power
+    return pool
+
+
+def alike(a, b):
+    for x, y in zip(a, b):
+        bits = torch.int16 if x.dtype == torch.bfloat16 else torch.int32
+        assert torch.equal(x.view(bits), y.view(bits)), (x.float() - y.float()).abs().max()
+
+
+# as in test_gpu_attn_cache_scored.py, then cap, slope, window, sink, span
+SCORED = [
+    ((3, 10, 2, 128, 1, 9, [1, 65, 570], None, False, False, "bf16"), 30.0, False, 0, 0, None),
+    ((2, 6, 2, 64, 5, 5, [130, 300], [5, 3], True, False, "bf16"), 30.0, True, 17, 3, None),
+    ((2, 4, 2, 64, 20, 6, [380, 333], [20, 7], False, False, "bf16"), 15.0, False, 0, 0, "holes"),
+    ((2, 2, 1, 64, 130, 5, [310, 260], [130, 40], False, False, "bf16"), 30.0, False, 0, 0, None),
+    ((2, 2, 1, 64, 130, 5, [250, 130], [130, 77], True, False, "bf16"), 30.0, True, 65, 1, None),
+    ((1, 2, 1, 128, 150, 9, [560], [100], False, False, "bf16"), 300.0, True, 0, 5, "holes"),
+    ((1, 1, 1, 128, 140, 12, [760], [130], True, False, "bf16"), 0.0, True, 150, 130, None),
+    ((1, 2, 1, 64, 140, 6, [370], [90], False, False, "f32"), 30.0, True, 0, 0, "holes"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(SCORED)))
+def test_scored_stale_places(i):
+    case, *rest = SCORED[i]
+    opt = options(case, *rest)
+    x = make(case)
+    unseen = ~seen(case, opt).any(1)
+    got = [run(case, filled(x[0], x[1], case[3], unseen, *s), x, opt) for s in STALE]
+    alike(got[0], got[1])
+    alike(got[0], got[2])

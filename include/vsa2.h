@@ -623,8 +623,8 @@ vsa2_status vsa2_cache_read(const vsa2_cache* c, int32_t dtype, int32_t n, const
  *   lse     [batch][heads_q][n] fp32 natural-log log-sum-exp.
  *   length  device int32 [batch] (clamped to [0, 64 max_pages]); count device
  *           int32 [batch] or NULL for n.
- *   A row with nothing to attend gets o = 0, lse = -inf.  What masked places and
- *   the pages' unwritten rest hold (NaN too) reaches no output.
+ *   A row with nothing to attend gets o = 0, lse = -inf.  What masked places, the
+ *   pages' unwritten rest and the queries of such rows hold (NaN too) reaches no output.
  *   ws, ws_bytes  workspace of vsa2_attn_cache_workspace bytes, 256-byte aligned:
  *           partial results of long lists, which are split over workgroups and
  *           joined in a fixed order.

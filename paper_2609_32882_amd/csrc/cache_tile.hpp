@@ -78,6 +78,19 @@ __device__ __forceinline__ void split_frag(frag_bf16* f, const float* x) {
     }
 }
 
+// Zeros instead of fragments.
+template <int N>
+__device__ __forceinline__ void zeros_if(bool no, frag_bf16* f) {
+    typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32x4_t;
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+        u32x4_t w = __builtin_bit_cast(u32x4_t, f[x].v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = no ? 0u : w[i];
+        f[x].v = __builtin_bit_cast(bf16x8_t, w);
+    }
+}
+
 // 8 probabilities times their powers: three bf16 terms, or fp16, whose rounding (2^-12 of a
 // weight at most, against the result's 2^-9) is the one to fewer bits before the result.
 template <int N>
@@ -897,7 +910,7 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
     mine <<= wave;
     const int32_t* list = list_of(a, b, h);
     const int early = !SC::ON && a.splits == 1 && lane < a.c.max_pages ? list[lane] : -1;
-    // rows that see nothing take what the others compute and drop it at the end
+    // rows that see nothing compute with queries of zeros, which leave the others alone, and drop it at the end
     typename SC::row row[XT];
     int lim_max = 0, lim_min = 0, pages;
     scored_ends ends;
@@ -941,6 +954,8 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
     for (int x = 0; x < XT; ++x) {
         const int r = tile * TR + x * TILE + col;
         const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset<KIND>(a.q, a, b, h, r) : 0);
+        // (read before it is known, so that lengths and queries are waited for together)
+        const bool dead = sees_nothing(row[x]);
 #pragma unroll
         for (int u = 0; u < D / 32; ++u) {
             float y[8] = {};
@@ -950,6 +965,7 @@ __device__ __forceinline__ void tile_body(const attn_args& a, const SC& sc, uint
                 for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
             }
             split_frag<NT>(qf[x][u], y);
+            zeros_if<NT>(dead, qf[x][u]);
         }
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) st[x].o[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -1401,6 +1417,7 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
     const int hi = static_cast<int>(static_cast<int64_t>(pages) * (split + 1) / a.splits);
 
     frag_bf16 qf[KC][2][NT];
+    const bool dead = sees_nothing(row);       // queries of zeros, which leave the others alone
     const T* q = static_cast<const T*>(a.q.ptr) + (r < a.rows ? row_offset<KIND>(a.q, a, b, h, r) : 0);
 #pragma unroll
     for (int w = 0; w < KC; ++w)
@@ -1413,6 +1430,7 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
                 for (int i = 0; i < 8; ++i) y[i] = to_f32(e[i]);
             }
             split_frag<NT>(qf[w][z], y);
+            zeros_if<NT>(dead, qf[w][z]);
         }
     rows_state<T, D> st;
     powers_seen seen;
@@ -1520,7 +1538,7 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[c][i] *= back;
     l += swap_half(l);
-    if (sees_nothing(row)) {
+    if (dead) {
         m = -INFINITY;
         l = 0.f;
 #pragma unroll

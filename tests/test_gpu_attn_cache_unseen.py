@@ -1,17 +1,20 @@
 """What no row sees reaches no bit of the attentions' results: equal calls on pools whose stale
-bytes differ (behind a list's end, between two rows' ranges) give equal outputs.  NaN there is
-tested elsewhere; these are finite bytes of other requests."""
+bytes differ (behind a list's end, between two rows' ranges), or with other queries in the places
+past a call's counts, give equal outputs.  NaN there is tested elsewhere; these are finite bytes
+and queries of other requests."""
 import pytest
 import torch
 
 import around_reference as ref
-from test_gpu_attn_cache import make
+import paper_2609_32882_amd as vsa2
+from test_gpu_attn_cache import gpu, make
 from test_gpu_attn_cache_scored import options, run, seen
 
 pytestmark = pytest.mark.gpu
 
 # (code, power) of stale places: a fresh page's zeros, the largest finite code, sizes as real ones have
 STALE = [(0x00, 0), (0x7e, 150), (0xb1, 118)]
+SIZES = (0.0, 1.0, 2.0 ** 12, float("nan"))          # of queries past the counts
 
 
 def filled(pool, table, D, unseen, code, power):
@@ -25,6 +28,15 @@ def filled(pool, table, D, unseen, code, power):
             for x, at in enumerate(ref.offsets(pos % 64, D)):
                 pool[page, h, at] = code if x < 2 else power
     return pool
+
+
+def padded(q, counts, size):
+    """Queries with those past the counts (None: none) multiplied by size."""
+    q = q.clone()
+    for b in range(q.shape[0]):
+        if counts is not None:
+            q[b, :, int(counts[b]):] *= size
+    return q
 
 
 def alike(a, b):
@@ -55,3 +67,38 @@ def test_scored_stale_places(i):
     got = [run(case, filled(x[0], x[1], case[3], unseen, *s), x, opt) for s in STALE]
     alike(got[0], got[1])
     alike(got[0], got[2])
+
+
+@pytest.mark.parametrize("i", [i for i, c in enumerate(SCORED) if c[0][7]])
+def test_scored_padded_queries(i):
+    case, *rest = SCORED[i]
+    opt = options(case, *rest)
+    x = make(case)
+    got = [run(case, x[0], (*x[:2], padded(x[2], x[4], size), *x[3:]), opt) for size in SIZES]
+    for other in got[1:]:
+        alike(got[0], other)
+
+
+PLAIN = [
+    (2, 10, 2, 128, 1, 5, [65, 290], None, False, False, "bf16"),
+    (2, 4, 2, 64, 20, 4, [150, 210], [20, 5], False, False, "bf16"),
+    (1, 1, 1, 64, 140, 4, [150], None, False, False, "bf16"),
+    (2, 2, 1, 128, 140, 6, [150, 280], [140, 100], False, False, "bf16"),
+    (1, 2, 2, 128, 150, 4, [200], None, True, False, "bf16"),
+    (1, 2, 1, 64, 140, 6, [330], [70], False, False, "f32"),
+]
+
+
+
+
+@pytest.mark.parametrize("i", [i for i, c in enumerate(PLAIN) if c[7]])
+def test_padded_queries(i):
+    case = PLAIN[i]
+    pool, table, q, length, count = make(case)
+    cache = vsa2.KVCache(pool.cuda(), table.cuda())
+    prefix = vsa2.KVCache(cache.pool, table[:1].contiguous().cuda())          # the first list as the one that all share
+    for call in (lambda y: vsa2.attn_cache(cache, y, length.cuda(), gpu(count), causal=case[8]),
+                 lambda y: vsa2.attn_cache_shared(prefix, cache, y, length[:1].cuda(), length.cuda(), gpu(count), causal=case[8])):
+        got = [call(padded(q, count, size).cuda()) for size in SIZES]
+        for other in got[1:]:
+            alike(got[0], other)

@@ -1088,7 +1088,7 @@ __device__ __forceinline__ void rows_move(const f32x16_t (&s)[N], const float (*
     if (__ballot(far) == 0) return;
     const float up = fmaxf(st.w.base + st.w.lift(), mx * scale);
     float most = fmaf(mx, scale, -up) - 7.f;
-    bool wide = false;          // a lane's token of each page more than 2^7 below E (past a limit: whatever)
+    bool wide = false;          // a lane's token of each page more than 2^7 below E (or past all limits)
     if constexpr (LIFTED) {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) wide |= power[i][1][lane_id()] < 1.f;
@@ -1489,7 +1489,11 @@ __device__ __forceinline__ void rows_body(const attn_args& a, const SC& sc, uint
 #pragma unroll
             for (int x = 0; x < STAGE; ++x) {
                 if constexpr (SC::ON) marked |= (mine[x] & ve[x]) << (8 * x);
-                else if (x < have && pos[x] * CACHE_TOKENS + lane < wmax) marked |= static_cast<uint32_t>(ve[x]) << (8 * x);
+                else {
+                    // past the wave's limits whatever the page holds: a power of 0, as on a page of zeros
+                    if (x >= have || pos[x] * CACHE_TOKENS + lane >= wmax) ve[x] = 0;
+                    marked |= static_cast<uint32_t>(ve[x]) << (8 * x);
+                }
             }
             seen.look(marked);
         }

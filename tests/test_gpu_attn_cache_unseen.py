@@ -79,6 +79,28 @@ def test_scored_padded_queries(i):
         alike(got[0], other)
 
 
+def steep(case, seed=3):
+    """Like make(): the tokens of a list's last page have value rows 2^20 times those before it, and every
+    row scores them some 12 below, so that the scale of the weights moves there and rows are lifted."""
+    batch, hq, hkv, D, n, max_pages, lengths, counts, causal, lists, dtype = case
+    pool, table, q, length, count = make(case, seed)
+    g = torch.Generator().manual_seed(seed)
+    u = torch.randn(D, generator=g)
+    u *= D ** 0.25 / u.norm()                                   # u.u / sqrt(D) = 1
+    m = max(lengths)
+    k = 0.2 * torch.randn(batch, hkv, m, D, generator=g)
+    v = torch.randn(batch, hkv, m, D, generator=g)
+    for b in range(batch):
+        last = (lengths[b] - 1) // 64 * 64
+        k[b, :, :last] += 2 * u
+        k[b, :, last:] -= 10 * u
+        v[b, :, :last] *= 2.0 ** -10
+        v[b, :, last:] *= 2.0 ** 10
+    ref.write_reference(pool, table, k, v, [0] * batch, lengths)
+    q = (u + 0.2 * torch.randn(batch, n, hq, D, generator=g)).to(q.dtype).transpose(1, 2)
+    return pool, table, q, length, count
+
+
 PLAIN = [
     (2, 10, 2, 128, 1, 5, [65, 290], None, False, False, "bf16"),
     (2, 4, 2, 64, 20, 4, [150, 210], [20, 5], False, False, "bf16"),
@@ -102,3 +124,19 @@ def test_padded_queries(i):
         got = [call(padded(q, count, size).cuda()) for size in SIZES]
         for other in got[1:]:
             alike(got[0], other)
+
+
+@pytest.mark.parametrize("i", range(len(PLAIN)))
+@pytest.mark.parametrize("data", [make, steep])
+def test_stale_places(i, data):
+    case = PLAIN[i]
+    pool, table, q, length, count = data(case)
+    unseen = torch.arange(case[5] * 64) >= length[:, None]
+    caches = [vsa2.KVCache(filled(pool, table, case[3], unseen, *s).cuda(), table.cuda()) for s in STALE]
+    first = table[:1].contiguous().cuda()                    # the first list as the one that all share
+    for call in (lambda c: vsa2.attn_cache(c, q.cuda(), length.cuda(), gpu(count), causal=case[8]),
+                 lambda c: vsa2.attn_cache_shared(vsa2.KVCache(c.pool, first), c, q.cuda(), length[:1].cuda(), length.cuda(),
+                                                  gpu(count), causal=case[8])):
+        got = [call(c) for c in caches]
+        alike(got[0], got[1])
+        alike(got[0], got[2])

@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cfloat>
 #include <exception>
 #include <string>
 
@@ -462,7 +463,9 @@ PyObject* attn_cache_scored(PyObject* const* a, Py_ssize_t n) {
     const vsa2_cache& c = *structure<vsa2_cache>(a[0], "cache");
     attn_rows r(c, a[1], a[10]);
     vsa2_scores sc;
-    sc.cap = static_cast<float>(real(a[5]));
+    const double cap = real(a[5]);
+    sc.cap = static_cast<float>(cap);
+    if (sc.cap == 0.f && cap != 0.) sc.cap = FLT_MIN;         // no cap is 0 itself; this one the library refuses
     sc.slope = contiguous<float>(tensor(a[6], "slope"), {r.heads}, at::kFloat, "slope");
     sc.window = integer32(a[7], "window");
     sc.sink = integer32(a[8], "sink");

@@ -2,8 +2,8 @@
 // how often a page is held, and copies of tokens between lists.
 //
 // Assigning lists is index work, bound by the latency of launches and of loads that wait
-// for one another, unless pages are copied.  One workgroup does it where the lists fit its
-// LDS: it saves the old lists, gives up their pages, writes the new lists, settles who
+// for one another, unless pages are copied.  One workgroup does it where lists are short, in
+// its LDS: it saves the old lists, gives up their pages, writes the new lists, settles who
 // copies a shared last page, numbers the requests for pages in order of the sequences, and
 // hands out the free pages in order of their index; a second launch copies pages.  Longer
 // lists are moved by launches of their own, larger pools searched by a workgroup for every
@@ -22,9 +22,16 @@ namespace {
 constexpr int NT = 1024;                 // threads of the planning workgroup
 constexpr int PER = 16;                  // pages a thread looks at in a step
 constexpr int STEP = NT * PER;           // pages of a step
-constexpr int LONE_STEPS = 4;            // steps that one workgroup takes alone
-constexpr int LONE_ENTRIES = 24576;      // list entries that it keeps in LDS
-constexpr int LONE_FORKS = 2048;         // and where sequences take others' lists
+// One workgroup alone against several launches, us a call with a token for every list, in pools with
+// room at their start: 64 lists of 32, 48, 64, 128 and 384 pages that stay 8.9 9.1 10.0 13.2 26.2
+// against 9.6 9.3 9.7 10.7 15.2; that take others' lists, of 32, 64, 80, 96 and 128 pages 9.9 11.2 11.5
+// 12.4 13.8 against 11.4 12.2 12.2 12.4 13.0; that lose pages, of 96 and 128 11.7 13.3 against 12.6 13.4;
+// both, of 96 and 128 12.5 13.9 against 14.3 14.8.
+constexpr int LONE_TRIMS = 3072;         // list entries of a workgroup alone where they stay in their places
+constexpr int LONE_ENTRIES = 6144;       // and where lists take others' or lose pages
+// Free pages at the end of pools of 4, 5, 8 and 16 steps: 17.2 19.6 26.7 45.4 by a workgroup alone, against
+// 17.5 18.4 18.5 18.1 with a workgroup for every step.
+constexpr int LONE_STEPS = 4;            // steps that one workgroup searches alone
 
 enum last_page { NONE, KEEPS, COPIES, STUCK };      // what a sequence does about its shared last page
 
@@ -107,7 +114,11 @@ __global__ __launch_bounds__(256) void lists_write_kernel(assign_args a) {
 }
 
 // Lists that go on from others' without losing pages: entries stay in their columns, so a workgroup
-// that holds some columns of all lists saves and writes them in one launch.
+// that holds some columns of all lists saves and writes them in one launch.  With 128 workgroups at
+// least, where there are as many columns, against saved and written lists (us): 64 lists of 100, 200
+// and 512 pages 12.8 14.2 13.3 against 14.4 16.1 15.0, 32 of 2,000 14.2 against 15.1, 4 of 8,000 10.8
+// against 13.6, but 500 of 40 18.3 against 17.4; 512 workgroups 12.8 15.9 18.4, 14.7, 11.2, 32 of them
+// 11.8 14.7 16.9, 20.4, 14.2.
 constexpr int COLUMN_ENTRIES = 8192;
 __global__ __launch_bounds__(256) void lists_columns_kernel(assign_args a, int columns) {
     __shared__ int old[COLUMN_ENTRIES];
@@ -326,8 +337,8 @@ __global__ __launch_bounds__(NT) void lists_alone_kernel(assign_args a) {
     __shared__ seq_info info[NT];
     __shared__ list_move moves[NT];
     __shared__ wg_sums sums;
-    __shared__ int old[LONE_ENTRIES];
-    static_assert(LONE_ENTRIES >= STEP, "the free pages of a step go there, too");
+    __shared__ int old[STEP];
+    static_assert(LONE_ENTRIES <= STEP, "the lists' entries, then the free pages of a step");
     const int tid = threadIdx.x, m = a.c.max_pages, all = a.c.batch * m;
     const float per = 1.f / static_cast<float>(m);
     bool inside = false;
@@ -642,14 +653,13 @@ hipError_t launch_cache_assign(int D, const cache_view& c, int32_t* table, int32
     w += up256(static_cast<size_t>(steps_of(c.pages)) * sizeof(int32_t));
     a.totals = reinterpret_cast<int32_t*>(w);
     const int64_t entries = static_cast<int64_t>(c.batch) * c.max_pages, steps = steps_of(c.pages);
-    if (c.batch <= NT && entries <= (source ? LONE_FORKS : LONE_ENTRIES) && steps <= LONE_STEPS) {
+    if (c.batch <= NT && entries <= (source || drop ? LONE_ENTRIES : LONE_TRIMS) && steps <= LONE_STEPS) {
         hipLaunchKernelGGL(lists_alone_kernel, dim3(1), dim3(NT), 0, s, a);
     } else {
         const dim3 wide(static_cast<unsigned>(std::min<int64_t>((entries + 255) / 256, 4096)));
         if (source && !drop && c.batch * 4 <= COLUMN_ENTRIES) {
-            // at least a column for every two of the 256 CUs
             const int columns = static_cast<int>(std::max<int64_t>(
-                1, std::min<int64_t>(COLUMN_ENTRIES / c.batch, (c.max_pages + 511) / 512)));
+                1, std::min<int64_t>(COLUMN_ENTRIES / c.batch, (c.max_pages + 127) / 128)));
             hipLaunchKernelGGL(lists_columns_kernel, dim3(static_cast<unsigned>((c.max_pages + columns - 1) / columns)), dim3(256),
                                0, s, a, columns);
         } else if (source || drop) {

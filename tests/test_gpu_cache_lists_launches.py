@@ -11,10 +11,11 @@ pytestmark = pytest.mark.gpu
 PAGE_BYTES = 128 * 64 + 128
 
 # batch, max_pages, pages of the pool, lists taken from others, pages left out.  One workgroup takes up to 1,024
-# sequences with 24,576 entries (2,048 where lists are taken from others) in a pool of 65,536 pages.
+# sequences with 6,144 entries (3,072 where they stay in their places) in a pool of 65,536 pages.
 CASES = [
     (40, 700, 3000, False, False), (40, 700, 3000, False, True),                # trimmed; saved and written
-    (40, 60, 500, True, False), (40, 60, 500, True, True),                      # by columns; saved and written
+    (40, 180, 1500, True, False), (40, 180, 1500, True, True),                  # by columns; saved and written
+    (40, 60, 500, True, False), (40, 60, 500, True, True), (40, 60, 500, False, True),      # one workgroup
     (1100, 3, 1500, True, False), (1100, 3, 1500, True, True), (1100, 3, 1500, False, False),
     (2500, 2, 1300, True, False),                                               # too many for columns
     (30, 5, 65600, False, False), (30, 5, 65600, True, True), (1030, 3, 65600, True, False),
@@ -66,12 +67,11 @@ def test_matches_the_plain_form(case, seed):
     assert torch.equal(pool[:, 0].amin(1).cpu(), small[:, 0, 0]) and torch.equal(pool[:, 0].amax(1).cpu(), small[:, 0, 0])
 
 
-@pytest.mark.parametrize("batch,pages", [(1100, 1500), (200, 65600), (900, 2100)])
+@pytest.mark.parametrize("batch,m,pages", [(1100, 3, 1500), (200, 3, 65600), (900, 3, 2100), (900, 7, 2100)])
 @pytest.mark.parametrize("free", [0, 1, 150])
-def test_a_shared_last_page_that_all_holders_write(batch, pages, free):
+def test_a_shared_last_page_that_all_holders_write(batch, m, pages, free):
     """Four pages, each the last one of a quarter of the sequences, two of them another table's, too: copies that
     are refused leave the page shared, and then its last holder, who needs none, has no room either."""
-    m = 3
     table = torch.full((batch, m), -1, dtype=torch.int32)
     table[:, 0] = pages // 2
     table[:, 1] = torch.arange(batch) % 4 * 7 + 11

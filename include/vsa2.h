@@ -647,8 +647,7 @@ vsa2_status vsa2_attn_cache(const vsa2_cache* c, int32_t dtype, int32_t heads_q,
  *   seen by token i of sequence b: prefix positions j < prefix_length[b / samples]
  *   and own positions j < limit, limit as in vsa2_attn_cache (causal there, too);
  *   nothing for i >= count[b].
- * The shared list is read and decoded once for tiles of the rows of all its
- * sequences.
+ * The shared list is read once for tiles of the rows of all its sequences.
  *   prefix  lists of prefix->batch groups, a divisor of c->batch; heads_kv and head_dim as
  *           c's; its pool may be c's or another.
  *   prefix_length  device int32 [prefix->batch]; length, count  as in vsa2_attn_cache.
@@ -667,7 +666,8 @@ vsa2_status vsa2_attn_cache_shared(const vsa2_cache* prefix, const vsa2_cache* c
 
 /*
  * vsa2_attn_cache_scored - vsa2_attn_cache with other scores and fewer positions.
- * With p = length[b] - count[b] + i, the list position of token i itself, and
+ * With p = length[b] - count[b] + i, the list position of token i itself (length and
+ * count as that call takes them: within [0, 64 max_pages] and [0, n]), and
  * x = q.k_j / sqrt(D), the softmax is over
  *   y = cap tanh(x / cap) - slope[h] |p - j|        (cap = 0: x; slope NULL: none)
  * of the positions j < limit (as in vsa2_attn_cache) with

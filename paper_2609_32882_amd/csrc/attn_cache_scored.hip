@@ -13,8 +13,8 @@
 //
 // One token each of 16 sequences over up to 38,400, 40/8 heads of 128, capped: 156 us, 5.3
 // TB/s, bound by memory as the plain attention.  1,792 tokens over the first 1,792 and the last
-// 8,960 positions, 12 heads, cap and bias: 210 us, 0.61 PFLOP/s, bound by vector instructions
-// beside the MFMAs (62% and 25% of a SIMD's cycles); a loop that goes back and forth between
+// 8,960 positions, 12 heads, cap and bias: 209 to 216 us with the card's clock, 0.6 PFLOP/s, bound by
+// vector instructions beside the MFMAs (61% and 25% of a SIMD's cycles); a loop that goes back and forth between
 // pages with and without masks, compiled for each, spilled 222 registers more and took 271.
 #include <algorithm>
 

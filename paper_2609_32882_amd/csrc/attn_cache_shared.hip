@@ -5,14 +5,15 @@
 // attention, every piece gives (O, m, l) of its rows, and the pieces of both are joined,
 //   O = sum 2^(m_x - m) O_x / sum 2^(m_x - m) l_x,   m = max m_x.
 // A piece of the shared list serves the rows of all sequences that share it, so the list is
-// read and decoded once for tiles of 16, 32 or 128 of them and not once a
-// sequence.  Both lists' pieces are workgroups of one launch, the shared ones first: they
+// read once for tiles of 16, 32 or 128 of them and not once a sequence.  Each wave decodes what
+// it reads: a page once for a tile of 16 or 32 rows, whose waves take pages in turn, and four times
+// for 128, whose waves take 32 rows of the same page each.  Both lists' pieces are workgroups of one launch, the shared ones first: they
 // are bound by instructions where there are many rows and the own lists' by memory.
 //
 // One token of each of 32 samples over 35,840 shared and up to 2,048 own tokens, 40/8 heads of
-// 128: 59 us; the plain attention over tables that all name the shared pages takes 157.  Two
-// samples' frames of 1,792 tokens over 35,840 and 3,584, 12 heads: 933 us, 0.93 PFLOP/s, the plain
-// attention so 895: their rows fill the tiles either way, and the partial results' way to memory
+// 128: 59 to 64 us with the card's clock; the plain attention over tables that all name the shared
+// pages takes 159 where this takes 64.  Two samples' frames of 1,792 tokens over 35,840 and 3,584, 12
+// heads: 927 to 968 us, 0.9 PFLOP/s, the plain attention so 926 where this takes 967: their rows fill the tiles either way, and the partial results' way to memory
 // is not needed there.  Tried: a tile's walk over the shared list and then its own as one list
 // (frames 954 us), the next page's keys requested during a page's softmax, into the registers
 // that its scores leave free (59.2 and 59.4 us; D = 64 18.2 and 19.1).
@@ -141,7 +142,11 @@ __global__ __launch_bounds__(SLICES > 8 ? 32 * SLICES : 256) void shared_join_ke
 // What a workgroup's piece of `pages` takes, in us: a start and an end, then its pages, which
 // tiles' waves share out and rows' waves walk together.  Measured with two workgroups a CU (one
 // alone is faster by a third): 35,840 shared tokens, 8 heads of 128, 160 rows in pieces for 160
-// to 1,000 workgroups 45 to 67 us, this with 18 us around it within 4 of them.
+// to 1,000 workgroups 45 to 67 us, this with 18 us around it within 4 of them.  A page of D = 64, or of
+// fp32 rows, takes other times, but all pieces' alike: of 56 pairs of numbers of pieces from 2 to 256 and
+// 1 to 8 the rule's was within 1% of the fastest in seven calls (32 tokens over 35,840, D = 64: bf16 41.6 us,
+// best 41.8, fp32 56.1 and 55.5, fp32 of D = 128 89.4 and 91.1; D = 64, 2 x 8 tokens over 20,000 18.3 and
+// 18.2, 4 x 16 over 8,000 21.1 and 21.2, 600 rows over 20,000 63.3 and 62.9; fp32, 64 over 17,000 27.4 and 27.4).
 double piece_time(const side_plan& p, int dtype, int64_t pages, bool pairs) {
     const int64_t n = (pages + p.splits - 1) / p.splits;
     const double page = p.tile_rows == ROWS ? 2.4 : (pairs ? 2. : 1.5);

@@ -320,8 +320,8 @@ struct scored_ends {
 // x = s * scale.
 //
 // tanh(y) = 1 - 2 / (e^2y + 1), or, below 0.5, the odd polynomial y + a y^3 + b y^5 + c y^7 that is
-// nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most): s times a
-// polynomial of s^2.  Where all of a wave's scores that some row sees are small only that is worked
+// nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most, of a score by
+// 2^-22.3 of the cap and by 2^-19.9 of itself): s times a polynomial of s^2.  Where all of a wave's scores that some row sees are small only that is worked
 // out, the bias added by the same instructions.  Elsewhere the first serves all of the wave's scores
 // up to caps of 2^8, off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a
 // score takes the one that is its own above, where small ones would lose bits (0.08 of a score of 1
@@ -330,8 +330,8 @@ struct scored_ends {
 // them bits (cap 50: 2^-17 of the weights).  A page behind all rows' own positions, or more than a
 // page before them, has a bias that is linear in the position; nearer ones take distances as whole
 // numbers, so that an own position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128:
-// 150 us without options (plain attention 152), 161 with a bias, 183 with a cap that the polynomial
-// serves, 202 with one that it does not (by it alone the capped frame of attn_cache_scored.hip went
+// 148 us without options (plain attention 144), 165 with a bias, 185 with a cap that the polynomial
+// serves, 203 with one that it does not, 193 with the first cap and a bias (by it alone the capped frame of attn_cache_scored.hip went
 // from 222 to 212 us).
 template <bool EXACT>
 struct score_form {

@@ -4,19 +4,21 @@
 // softmax over both lists together: each is cut into pieces as in the plain
 // attention, every piece gives (O, m, l) of its rows, and the pieces of both are joined,
 //   O = sum 2^(m_x - m) O_x / sum 2^(m_x - m) l_x,   m = max m_x.
-// A piece of the shared list serves the rows of all sequences that share it, so the list is
-// read once for tiles of 16, 32 or 128 of them and not once a sequence.  Each wave decodes what
-// it reads: a page once for a tile of 16 or 32 rows, whose waves take pages in turn, and four times
-// for 128, whose waves take 32 rows of the same page each.  Both lists' pieces are workgroups of one launch, the shared ones first: they
-// are bound by instructions where there are many rows and the own lists' by memory.
+// A piece of the shared list serves the rows of all sequences that share it, so the list is read
+// once for tiles of 16, 32 or 128 of them and not once a sequence.  Each wave decodes what it
+// reads: a page once for a tile of 16 or 32 rows, whose waves take pages in turn, and four times
+// for 128, whose waves take 32 rows of the same page each.  Both lists' pieces are workgroups of
+// one launch, the shared ones first: they are bound by instructions where there are many rows and
+// the own lists' by memory.
 //
-// One token of each of 32 samples over 35,840 shared and up to 2,048 own tokens, 40/8 heads of
-// 128: 59 to 64 us with the card's clock; the plain attention over tables that all name the shared
-// pages takes 159 where this takes 64.  Two samples' frames of 1,792 tokens over 35,840 and 3,584, 12
-// heads: 927 to 968 us, 0.9 PFLOP/s, the plain attention so 926 where this takes 967: their rows fill the tiles either way, and the partial results' way to memory
-// is not needed there.  Tried: a tile's walk over the shared list and then its own as one list
-// (frames 954 us), the next page's keys requested during a page's softmax, into the registers
-// that its scores leave free (59.2 and 59.4 us; D = 64 18.2 and 19.1).
+// One token of each of 32 samples over 35,840 shared and up to 2,048 own tokens, 40/8 heads of 128:
+// 59 to 64 us with the card's clock; the plain attention over tables that all name the shared pages
+// takes 159 where this takes 64.  Two samples' frames of 1,792 tokens over 35,840 and 3,584, 12
+// heads: 927 to 968 us, 0.9 PFLOP/s, the plain attention so 926 where this takes 967: their rows
+// fill the tiles either way, and the partial results' way to memory is not needed there.  Tried: a
+// tile's walk over the shared list and then its own as one list (frames 954 us), the next page's
+// keys requested during a page's softmax, into the registers that its scores leave free (59.2 and
+// 59.4 us; D = 64 18.2 and 19.1).
 #include <algorithm>
 
 #include "cache_tile.hpp"

@@ -320,19 +320,20 @@ struct scored_ends {
 // x = s * scale.
 //
 // tanh(y) = 1 - 2 / (e^2y + 1), or, below 0.5, the odd polynomial y + a y^3 + b y^5 + c y^7 that is
-// nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most, of a score by
-// 2^-22.3 of the cap and by 2^-19.9 of itself): s times a polynomial of s^2.  Where all of a wave's scores that some row sees are small only that is worked
-// out, the bias added by the same instructions.  Elsewhere the first serves all of the wave's scores
-// up to caps of 2^8, off by 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a
-// score takes the one that is its own above, where small ones would lose bits (0.08 of a score of 1
-// at a cap of 2^20); that for all caps took 238 us of the capped frame below instead of 202.  fp32
-// queries take scores below 0.4 by the series instead, the others as above: the difference would cost
-// them bits (cap 50: 2^-17 of the weights).  A page behind all rows' own positions, or more than a
-// page before them, has a bias that is linear in the position; nearer ones take distances as whole
-// numbers, so that an own position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128:
-// 148 us without options (plain attention 144), 165 with a bias, 185 with a cap that the polynomial
-// serves, 203 with one that it does not, 193 with the first cap and a bias (by it alone the capped frame of attn_cache_scored.hip went
-// from 222 to 212 us).
+// nearest to it there (by linear programming over 3,001 points; off by 2^-22.3 at most, of a score
+// by 2^-22.3 of the cap and by 2^-19.9 of itself): s times a polynomial of s^2.  Where all of a
+// wave's scores that some row sees are small only that is worked out, the bias added by the same
+// instructions.  Elsewhere the first serves all of the wave's scores up to caps of 2^8, off by
+// 2^-22 of the cap (2^-14: a sixty-fourth of the result's rounding), and a score takes the one that
+// is its own above, where small ones would lose bits (0.08 of a score of 1 at a cap of 2^20); that
+// for all caps took 238 us of the capped frame below instead of 202.  fp32 queries take scores
+// below 0.4 by the series instead, the others as above: the difference would cost them bits (cap
+// 50: 2^-17 of the weights).  A page behind all rows' own positions, or more than a page before
+// them, has a bias that is linear in the position; nearer ones take distances as whole numbers, so
+// that an own position has no bias at all.  1,792 tokens over 10,752, 12 heads of 128: 148 us
+// without options (plain attention 144), 165 with a bias, 185 with a cap that the polynomial
+// serves, 203 with one that it does not, 193 with the first cap and a bias (by the polynomial the
+// capped frame of attn_cache_scored.hip went from 222 to 212 us).
 template <bool EXACT>
 struct score_form {
     float scale, cap, rate;      // scale times log2 e, cap times log2 e, exponent of a score

@@ -27,7 +27,7 @@ constexpr int STEP = NT * PER;           // pages of a step
 // against 9.6 9.3 9.7 10.7 15.2; that take others' lists, of 32, 64, 80, 96 and 128 pages 9.9 11.2 11.5
 // 12.4 13.8 against 11.4 12.2 12.2 12.4 13.0; that lose pages, of 96 and 128 11.7 13.3 against 12.6 13.4;
 // both, of 96 and 128 12.5 13.9 against 14.3 14.8.
-constexpr int LONE_TRIMS = 3072;         // list entries of a workgroup alone where they stay in their places
+constexpr int LONE_TRIMS = 3400;         // list entries of a workgroup alone where they stay in their places
 constexpr int LONE_ENTRIES = 6144;       // and where lists take others' or lose pages
 // Free pages at the end of pools of 4, 5, 8 and 16 steps: 17.2 19.6 26.7 45.4 by a workgroup alone, against
 // 17.5 18.4 18.5 18.1 with a workgroup for every step.

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 PAGE_BYTES = 128 * 64 + 128
 
 # batch, max_pages, pages of the pool, lists taken from others, pages left out.  One workgroup takes up to 1,024
-# sequences with 6,144 entries (3,072 where they stay in their places) in a pool of 65,536 pages.
+# sequences with 6,144 entries (3,400 where they stay in their places) in a pool of 65,536 pages.
 CASES = [
     (40, 700, 3000, False, False), (40, 700, 3000, False, True),                # trimmed; saved and written
     (40, 180, 1500, True, False), (40, 180, 1500, True, True),                  # by columns; saved and written
